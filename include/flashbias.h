@@ -324,6 +324,82 @@ int fb_lowrank_xattn_bwd(const void* q, const void* k, const void* v,
 int fb_fold_batch(const void* src0, void* dst0, long long n0, const void* src1, void* dst1, long long n1, int B,
                   fb_dtype dtype, void* stream);
 
+/*
+ * Rotary positions with up to four axes (text; rows and columns; time, rows and columns): pair p of a row is turned by
+ * theta = positions[axis(p)] * freqs[p],
+ *     y1 = x1 cos(theta) - x2 sin(theta),   y2 = x2 cos(theta) + x1 sin(theta).
+ * sections[4] (host memory): how many pairs belong to axis 0, 1, 2, 3, in this order; P = their sum, 1 <= P <= C / 2.  Pair p
+ * is the channels (p, P + p), or (2 p, 2 p + 1) when interleaved; channels from 2 P on are copied.
+ *   x0 [B,H0,N,C] and, with H1 > 0, x1 [B,H1,N,C] (queries and the keys of grouped heads in one call): strides[6] (host
+ *   memory) holds their batch, head and row strides in elements, channels adjacent, so that slices of a fused projection
+ *   are read as they are; any start of a row, aligned to the element.  y0, y1: contiguous, 16-byte aligned; y may be x where x is
+ *   contiguous too, else they must not overlap.
+ *   positions [axes, Bp, N] (axes: up to the last section that is not 0), float when positions_f32, else int; Bp = 1 when
+ *   positions_shared, else B.  freqs [P] float, radians per position.  Angles are formed in 64 bits (exact product of the
+ *   two values as stored), so far positions keep theirs.  dtype FB_BF16 or FB_F32; C as everywhere.
+ * fb_rotary_bwd turns back: dx from the gradient dy, same arguments (positions and frequencies are constants).
+ */
+int fb_rotary_fwd(const void* x0, void* y0, int H0, const void* x1, void* y1, int H1, const long long* strides,
+                  const void* positions, int positions_f32, int positions_shared, const float* freqs, const int* sections,
+                  int B, int N, int C, int interleaved, fb_dtype dtype, void* stream);
+
+int fb_rotary_bwd(const void* dy0, void* dx0, int H0, const void* dy1, void* dx1, int H1, const long long* strides,
+                  const void* positions, int positions_f32, int positions_shared, const float* freqs, const int* sections,
+                  int B, int N, int C, int interleaved, fb_dtype dtype, void* stream);
+
+/*
+ * Pages of a key-value cache.  The cache of a layer is k_pages, v_pages [n_pages, Hkv, page, C] and, for a low-rank bias,
+ * phi_pages [n_pages, Hkv, page, R]; page in {16, 32, 64, 128, 256}, n_pages * page < 2^31.  Request b of a batch of B holds
+ * lens[b] tokens; token t lies in row t % page of page table[b, t / page] (table [B, max_blocks]), its slot is
+ * table[b, t / page] * page + t % page.  All of these are int arrays in device memory, one table for all layers.
+ *
+ * fb_paged_plan moves the requests from lens to new_lens tokens and maps the new ones:
+ *   ring [n_pages], state [2]: the free pages are ring[(state[0] + i) % n_pages], 0 <= i < state[1].
+ *   Requests that shrink (to 0: they have ended) give their last pages back, to the end of the ring, in the order (b, block);
+ *   then requests that grow take theirs from its head in the order of b: request b gets its pages if the pages that requests
+ *   0..b need add up to no more than are free.  One that does not, one whose new length exceeds max_blocks * page, or that grows
+ *   by more than N tokens, keeps its length; its slots are -1.  Negative lengths count as 0.
+ *   lens_out [B], state_out [2]: lengths and free pages afterwards (not in place).  table and ring are updated in place;
+ *   table entries behind a request's last page keep what they held.  slots [B, N]: slot of the request's i-th new token, -1
+ *   behind the last; positions [B, N] or NULL: its position in the request, 0 behind the last.
+ *   B <= 4096.  A page must be owned once: in the ring or by one request.  An entry that is no page gives slot -1.
+ */
+int fb_paged_plan(const int* lens, const int* new_lens, int* table, int* ring, const int* state,
+                  int* lens_out, int* state_out, int* slots, int* positions,
+                  int B, int N, int page, int n_pages, int max_blocks, void* stream);
+
+/*
+ * Stores the new tokens' rows k, v [B,Hkv,N,C] (strides[6], host memory: batch, head and row strides of k, then of v, in
+ * elements, channels adjacent, any start aligned to the element) and phi_k [Bp,Hkv,N,R] (contiguous; R = 0: none) into their
+ * pages.  A slot outside [0, n_pages * page) stores nothing; the slots of a call must differ.  R <= 64.
+ */
+int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* slots,
+                    void* k_pages, void* v_pages, void* phi_pages, const long long* strides,
+                    int B, int Hkv, int N, int C, int R, int page, int n_pages,
+                    fb_dtype dtype, fb_dtype phi_dtype, int phi_batch_broadcast, void* stream);
+
+/*
+ * Attention of N new tokens per request over the pages (one in decode, a few when drafted tokens are checked): q, out
+ * [B,H,N,C], lse [B,H,N]; query head h reads key head h / (H / Hkv).  Bias: factors phi_q [Bp,H,N,R] against phi_pages (R <= 64),
+ * or ALiBi -slopes[h] (i - j) (slopes [H] float, R = 0), or none.
+ *   Query n of request b has the position i = starts[b] + n (starts NULL: lens[b] - N + n).  causal: it sees the keys
+ *   j <= i of the request and is no query at all when i lies outside [0, lens[b]); else it sees all lens[b] keys (states of an
+ *   encoder).  Keys in a table entry that is no page are not seen; lens are cut to [0, max_blocks * page].  What lies in the pages behind the
+ *   last token, or in rows a query does not see, never reaches the result.  A query that sees nothing, or scores of -infinity
+ *   only, has out = 0 and lse = -infinity.
+ *   dtype FB_BF16 (products in bf16, probabilities in two bf16 limbs, everything else fp32) or FB_F32 (all fp32, fp32 factors).
+ *   workspace: device scratch of fb_paged_attn_fwd_workspace_bytes(...) bytes, 16-byte aligned, contents ignored, for the parts
+ *   of key heads that several workgroups share; without it (NULL, or too small) a key head stays in one workgroup.
+ */
+size_t fb_paged_attn_fwd_workspace_bytes(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype);
+
+int fb_paged_attn_fwd(const void* q, const void* k_pages, const void* v_pages,
+                      const void* phi_q, const void* phi_pages, const float* slopes,
+                      const int* table, const int* lens, const int* starts, void* out, float* lse,
+                      int B, int H, int Hkv, int N, int C, int R, int page, int n_pages, int max_blocks, int causal,
+                      fb_dtype dtype, fb_dtype phi_dtype, int phi_batch_broadcast, float scale,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

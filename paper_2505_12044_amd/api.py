@@ -28,7 +28,8 @@ EXPORTS = (
     "fb_lowrank_mulbias_attn_bwd_workspace_bytes", "fb_lowrank_mulbias_attn_bwd",
     "fb_alibi_attn_bwd_workspace_bytes", "fb_alibi_attn_bwd", "fb_lowrank_attn_bwd_noalloc",
     "fb_fold_batch", "fb_lowrank_xattn_fwd_workspace_bytes", "fb_lowrank_xattn_fwd_ws",
-    "fb_attn_bwd_call_workspace_bytes",
+    "fb_attn_bwd_call_workspace_bytes", "fb_rotary_fwd", "fb_rotary_bwd", "fb_paged_plan", "fb_paged_append",
+    "fb_paged_attn_fwd_workspace_bytes", "fb_paged_attn_fwd",
 )
 
 FB_STATIC_SCRATCH_BYTES = 64 << 20     # include/flashbias.h
@@ -98,6 +99,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fb_lowrank_xattn_fwd_ws.argtypes = [vp] * 7 + [ci] * 6 + [ci, ci, ci, cf, vp, sz, vp]
     lib.fb_fold_batch.restype = ci
     lib.fb_fold_batch.argtypes = [vp, vp, ctypes.c_longlong, vp, vp, ctypes.c_longlong, ci, ci, vp]
+    for f in (lib.fb_rotary_fwd, lib.fb_rotary_bwd):
+        f.restype = ci
+        f.argtypes = [vp, vp, ci] * 2 + [vp, vp, ci, ci, vp, vp] + [ci] * 5 + [vp]
+    lib.fb_paged_plan.restype = ci
+    lib.fb_paged_plan.argtypes = [vp] * 9 + [ci] * 5 + [vp]
+    lib.fb_paged_append.restype = ci
+    lib.fb_paged_append.argtypes = [vp] * 8 + [ci] * 10 + [vp]
+    lib.fb_paged_attn_fwd_workspace_bytes.restype = sz
+    lib.fb_paged_attn_fwd_workspace_bytes.argtypes = [ci] * 8
+    lib.fb_paged_attn_fwd.restype = ci
+    lib.fb_paged_attn_fwd.argtypes = [vp] * 11 + [ci] * 13 + [cf, vp, sz, vp]
     if path is None:
         _lib_handle = lib
     return lib
@@ -488,3 +500,187 @@ def fb_fold_batch(*grads, stream=None):
     st = lib.fb_fold_batch(_ptr(g0), o0.data_ptr(), n0, _ptr(g1), o1.data_ptr(), o1.numel(), B, dtype, _stream(stream))
     _check(st, "fb_fold_batch")
     return o0, o1
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise FlashBiasError(what)
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """All tensors of a call live on the current device, whose stream the call goes to."""
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != dev):
+            raise FlashBiasError("tensors must be CUDA tensors of the current device")
+
+
+def _ints(t: Optional[torch.Tensor], shape, name: str) -> None:
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise FlashBiasError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)}")
+
+
+_Six = ctypes.c_longlong * 6
+_Four = ctypes.c_int * 4
+
+
+def _row_strides(x: torch.Tensor, y: Optional[torch.Tensor]):
+    """Batch, head and row strides of one or two [B,H,N,C] tensors whose channels are adjacent."""
+    for t in (x, y):
+        if t is not None and (t.dim() != 4 or t.stride(3) != 1):
+            raise FlashBiasError("tensors must be [B,H,N,C] with adjacent channels")
+    return _Six(*x.stride()[:3], *(y.stride()[:3] if y is not None else (0, 0, 0)))
+
+
+def _rotary(lib_fn, what, x0, x1, positions, freqs, sections, interleaved, out, stream):
+    strides = _row_strides(x0, x1)
+    _here(x0, x1, positions, freqs, *(out or ()))
+    B, H0, N, C = x0.shape
+    sections = tuple(int(s) for s in sections)
+    _need(1 <= len(sections) <= 4, "one to four axes")
+    _need(x1 is None or (x1.dtype == x0.dtype and x1.shape[0] == B and tuple(x1.shape[2:]) == (N, C)),
+          "both tensors must have one dtype, batch, length and head dimension")
+    _need(positions.dtype in (torch.int32, torch.float32) and positions.is_contiguous() and positions.dim() == 3 and
+          positions.shape[0] == len(sections) and positions.shape[1] in (1, B) and positions.shape[2] == N,
+          "positions must be a contiguous int32 or float32 tensor [axes, B or 1, N]")
+    _need(freqs.dtype == torch.float32 and freqs.is_contiguous() and freqs.numel() == sum(sections),
+          "freqs must be a contiguous float32 tensor with one entry per pair")
+    if out is None:
+        out = (torch.empty((B, H0, N, C), dtype=x0.dtype, device=x0.device),
+               None if x1 is None else torch.empty((B, x1.shape[1], N, C), dtype=x0.dtype, device=x0.device))
+    y0, y1 = out
+    for x, y in ((x0, y0), (x1, y1)):
+        _need((x is None) == (y is None) and (x is None or (y.shape == x.shape and y.dtype == x.dtype)),
+              "outputs must have their inputs' shapes and dtype")
+    st = lib_fn(x0.data_ptr(), _ptr(y0), H0, None if x1 is None else x1.data_ptr(), _ptr(y1), 0 if x1 is None else x1.shape[1],
+                strides, positions.data_ptr(), int(positions.dtype == torch.float32), int(positions.shape[1] == 1),
+                freqs.data_ptr(), _Four(*sections), B, N, C, int(bool(interleaved)), _dtype_code(x0), _stream(stream))
+    _check(st, what)
+    return y0, y1
+
+
+def fb_rotary_fwd(q, k, positions, freqs, sections, interleaved: bool = False, out=None, stream=None):
+    """q [B,H,N,C] and k [B,Hkv,N,C] (or None) turned by their positions: pair p by positions[axis of p] * freqs[p] radians.
+    positions: [axes, B or 1, N] int32 or float32; freqs: float32, one per pair; sections: pairs of each axis, in order.
+    Pairs are the channels (p, P + p), P = sum(sections), or (2p, 2p + 1) when interleaved; other channels are copied.  q and k
+    may be slices of a fused projection (any strides with adjacent channels); the results are contiguous.  out: a pair of
+    contiguous tensors, q and k themselves where these are contiguous."""
+    return _rotary(load_library().fb_rotary_fwd, "fb_rotary_fwd", q, k, positions, freqs, sections, interleaved, out, stream)
+
+
+def fb_rotary_bwd(dq, dk, positions, freqs, sections, interleaved: bool = False, out=None, stream=None):
+    """The gradients of fb_rotary_fwd's q and k from those of its results (the inverse turn); same arguments."""
+    return _rotary(load_library().fb_rotary_bwd, "fb_rotary_bwd", dq, dk, positions, freqs, sections, interleaved, out, stream)
+
+
+def fb_paged_plan(lens, new_lens, table, ring, state, n_new: int, page: int, lens_out=None, state_out=None, slots=None,
+                  positions=None, stream=None):
+    """Moves B requests from lens to new_lens tokens: pages are given back and taken (table [B, max_blocks] and the ring of
+    free pages, int32, in place), and the up to n_new new tokens of each are mapped.  Returns lens [B] and state [2]
+    (ring head, free pages) afterwards, slots [B, n_new] (-1: no token) and positions [B, n_new]."""
+    lib = load_library()
+    B = lens.shape[0]
+    _here(lens, new_lens, table, ring, state, lens_out, state_out, slots, positions)
+    _ints(lens, (B,), "lens")
+    _ints(new_lens, (B,), "new_lens")
+    _need(table.dim() == 2, "table must be [B, max_blocks]")
+    _ints(table, (B, table.shape[1]), "table")
+    _ints(ring, (ring.numel(),), "ring")
+    _ints(state, (2,), "state")
+    new = lens.new_empty
+    lens_out = new((B,)) if lens_out is None else lens_out
+    state_out = new((2,)) if state_out is None else state_out
+    slots = new((B, n_new)) if slots is None else slots
+    positions = new((B, n_new)) if positions is None else positions
+    _ints(lens_out, (B,), "lens_out")
+    _ints(state_out, (2,), "state_out")
+    _ints(slots, (B, n_new), "slots")
+    _ints(positions, (B, n_new), "positions")
+    st = lib.fb_paged_plan(lens.data_ptr(), new_lens.data_ptr(), table.data_ptr(), ring.data_ptr(), state.data_ptr(),
+                           lens_out.data_ptr(), state_out.data_ptr(), slots.data_ptr(), positions.data_ptr(),
+                           B, n_new, page, ring.numel(), table.shape[1], _stream(stream))
+    _check(st, "fb_paged_plan")
+    return lens_out, state_out, slots, positions
+
+
+def _check_pages(k_pages, v_pages, phi_pages, R, phi_dtype):
+    _need(k_pages.dim() == 4 and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype,
+          "k_pages and v_pages must be [n_pages, Hkv, page, C] of one dtype")
+    _need((phi_pages is None) == (R == 0), "factors need their pages")
+    if R:
+        _need(tuple(phi_pages.shape) == (*k_pages.shape[:3], R) and phi_pages.dtype == phi_dtype,
+              "phi_pages must be [n_pages, Hkv, page, R] of the factors' dtype")
+
+
+def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, phi_batch_broadcast: Optional[bool] = None,
+                    stream=None) -> None:
+    """Stores k, v [B,Hkv,N,C] (any strides with adjacent channels) and phi_k [B or 1,Hkv,N,R] in the rows slots [B,N] of
+    k_pages, v_pages [n_pages,Hkv,page,C] and phi_pages [n_pages,Hkv,page,R].  Slots of -1 are left out; the others must differ."""
+    lib = load_library()
+    strides = _row_strides(k, v)
+    _here(k, v, slots, k_pages, v_pages, phi_k, phi_pages)
+    B, Hkv, N, C = k.shape
+    R = 0 if phi_k is None else phi_k.shape[-1]
+    _check_pages(k_pages, v_pages, phi_pages, R, None if phi_k is None else phi_k.dtype)
+    n_pages, hp, page, cp = k_pages.shape
+    _need(v.shape == k.shape and k.dtype == v.dtype == k_pages.dtype and (hp, cp) == (Hkv, C),
+          "k, v and their pages must have one dtype, head count and head dimension")
+    _need(R == 0 or (phi_k.shape[0] in (1, B) and tuple(phi_k.shape[1:]) == (Hkv, N, R)), "phi_k must be [B or 1,Hkv,N,R]")
+    _ints(slots, (B, N), "slots")
+    if phi_batch_broadcast is None:
+        phi_batch_broadcast = R > 0 and phi_k.shape[0] == 1 and B > 1
+    code = _dtype_code(k)
+    st = lib.fb_paged_append(k.data_ptr(), v.data_ptr(), _ptr(phi_k), slots.data_ptr(), _ptr(k_pages), _ptr(v_pages),
+                             _ptr(phi_pages), strides, B, Hkv, N, C, R, page, n_pages, code,
+                             _dtype_code(phi_k) if R else code, int(bool(phi_batch_broadcast)), _stream(stream))
+    _check(st, "fb_paged_append")
+
+
+def fb_paged_attn_fwd_workspace_bytes(B, H, Hkv, N, C, page, max_blocks, dtype_code=FB_BF16) -> int:
+    return int(load_library().fb_paged_attn_fwd_workspace_bytes(B, H, Hkv, N, C, page, max_blocks, dtype_code))
+
+
+def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None, phi_pages=None, slopes=None,
+                      causal: bool = True, scale: float = 0.0, out=None, lse=None,
+                      phi_batch_broadcast: Optional[bool] = None, workspace=None, stream=None):
+    """out, lse = attention of q [B,H,N,C], the N newest tokens of each request, over its pages: lens [B] keys each, the
+    first new token at position starts[b] (None: lens - N).  k_pages, v_pages [n_pages,Hkv,page,C], H a multiple of Hkv.
+    Bias: phi_q [B or 1,H,N,R] with phi_pages [n_pages,Hkv,page,R], or slopes [H] (ALiBi), or none.  causal=False: every
+    query sees all keys (an encoder's states).  Queries that see nothing get out = 0, lse = -inf.  Scratch of
+    fb_paged_attn_fwd_workspace_bytes: the caller's workspace, else the binding's own; a call that is given out and lse but no
+    workspace allocates nothing and does without (a key head is then not split over the GPU)."""
+    lib = load_library()
+    _here(q, k_pages, v_pages, table, lens, starts, phi_q, phi_pages, slopes, out, lse, workspace)
+    B, H, N, C = q.shape
+    R = 0 if phi_q is None else phi_q.shape[-1]
+    _check_pages(k_pages, v_pages, phi_pages, R, None if phi_q is None else phi_q.dtype)
+    n_pages, Hkv, page, cp = k_pages.shape
+    _need(k_pages.dtype == q.dtype and cp == C, "q and the pages must have one dtype and head dimension")
+    _need(R == 0 or (phi_q.shape[0] in (1, B) and tuple(phi_q.shape[1:]) == (H, N, R)), "phi_q must be [B or 1,H,N,R]")
+    _need(slopes is None or (slopes.dtype == torch.float32 and slopes.numel() == H),
+          "slopes must be a float32 tensor with one entry per head")
+    _need(table.dim() == 2, "table must be [B, max_blocks]")
+    blocks = table.shape[1]
+    _ints(table, (B, blocks), "table")
+    _ints(lens, (B,), "lens")
+    _ints(starts, (B,), "starts")
+    if phi_batch_broadcast is None:
+        phi_batch_broadcast = R > 0 and phi_q.shape[0] == 1 and B > 1
+    code = _dtype_code(q)
+    if workspace is None and (out is None or lse is None):
+        need = int(lib.fb_paged_attn_fwd_workspace_bytes(B, H, Hkv, N, C, page, blocks, code))
+        workspace = _scratch(need, q.device, stream) if need else None
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype and tuple(lse.shape) == (B, H, N) and lse.dtype == torch.float32,
+          "out must be like q, lse [B,H,N] float32")
+    st = lib.fb_paged_attn_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(phi_q), _ptr(phi_pages), _ptr(slopes),
+                               table.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr(),
+                               _ptr(out), _ptr(lse), B, H, Hkv, N, C, R, page, n_pages, blocks, int(bool(causal)),
+                               code, _dtype_code(phi_q) if R else code, int(bool(phi_batch_broadcast)), float(scale),
+                               _ptr(workspace), ws_bytes, _stream(stream))
+    _check(st, "fb_paged_attn_fwd")
+    return out, lse

@@ -138,6 +138,37 @@ class _DenseBias(torch.autograd.Function):
         return dq, dk, dv, _fold_batch(dbias, bias), None, None
 
 
+def _adjacent(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """Rows with adjacent channels are read as they lie (slices of a fused projection)."""
+    return t if t is None or t.stride(3) == 1 else t.contiguous()
+
+
+class _Rotary(torch.autograd.Function):
+    """Rotary positions; the backward turns the gradients back and keeps nothing of q and k."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, freqs, sections, interleaved):
+        ctx.save_for_backward(positions, freqs)
+        ctx.cfg = (sections, interleaved)
+        yq, yk = api.fb_rotary_fwd(_adjacent(q), _adjacent(k), positions, freqs, sections, interleaved=interleaved)
+        return yq if yk is None else (yq, yk)
+
+    @staticmethod
+    def backward(ctx, dq, dk=None):
+        positions, freqs = ctx.saved_tensors
+        sections, interleaved = ctx.cfg
+        dq, dk = api.fb_rotary_bwd(_adjacent(dq), _adjacent(dk), positions, freqs, sections, interleaved=interleaved)
+        return dq, dk, None, None, None, None
+
+
+def rotary_positions(q, k, positions, freqs, sections, interleaved: bool = False):
+    """q [B,H,N,C] and k [B,Hkv,N,C] (k may be None) turned by rotary positions of one to four axes; arguments as for
+    api.fb_rotary_fwd.  Differentiable in q and k; positions and freqs are constants.  Returns the pair (or q's alone)."""
+    if positions.requires_grad or freqs.requires_grad:
+        raise api.FlashBiasError("positions and freqs are constants: they receive no gradient")
+    return _Rotary.apply(q, k, positions, freqs, tuple(sections), bool(interleaved))
+
+
 def lowrank_bias_attention(q, k, v, phi_q=None, phi_k=None, causal: bool = False, scale: float = 0.0):
     """Attention with the additive bias phi_q phi_k^T.  q [B,H,N,C]; k, v [B,H,M,C]; phi_q [B or 1,H,N,R];
     phi_k [B or 1,H,M,R]; scale 0 means 1/sqrt(C).  Differentiable in q, k, v, phi_q, phi_k."""

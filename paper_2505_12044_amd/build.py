@@ -16,7 +16,8 @@ SOURCES = ["fb_api.hip", "fb_fwd_f32.hip", "fb_fwd_bf16.hip", "fb_fwd_bf16_c16.h
            "fb_fwd_bf16_c64.hip", "fb_fwd_bf16_c128.hip", "fb_fwd_bf16_alibi.hip", "fb_fwd_bf16_few.hip",
            "fb_fwd_bf16_short.hip",
            "fb_bwd_bf16.hip", "fb_bwd_bf16_short.hip", "fb_bwd_f32.hip",
-           "fb_mulbias.hip", "fb_fold.hip"]
+           "fb_mulbias.hip", "fb_fold.hip",
+           "fb_rotary.hip", "fb_paged.hip", "fb_paged_attn.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-ffast-math", "-fno-finite-math-only",

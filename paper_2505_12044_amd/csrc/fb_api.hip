@@ -611,5 +611,168 @@ int fb_fold_batch(const void* src0, void* dst0, long long n0, const void* src1, 
     return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
 }
 
+// ---- rotary positions, cache pages, attention over them ----
+static int elem_size(fb_dtype dtype) { return dtype == FB_F32 ? 4 : 2; }
+static bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (unsigned)(bytes - 1)) == 0; }
+static bool known(fb_dtype d) { return d == FB_F32 || d == FB_BF16; }
+
+static int rotary_impl(const void* x0, void* y0, int H0, const void* x1, void* y1, int H1, const long long* strides,
+                       const void* positions, int positions_f32, int positions_shared, const float* freqs, const int* sections,
+                       int B, int N, int C, int interleaved, fb_dtype dtype, int inverse, void* stream) {
+    if (!x0 || !y0 || !strides || !positions || !freqs || !sections) return FB_ERR_NULL;
+    if (H0 <= 0 || H1 < 0) return FB_ERR_SHAPE;
+    if (H1 > 0 && (!x1 || !y1)) return FB_ERR_NULL;
+    if ((long long)H0 + H1 > (1 << 30)) return FB_ERR_SHAPE;
+    if (int st = check_common(B, H0 + H1, N, C, 0)) return st;
+    if (!known(dtype)) return FB_ERR_UNSUPPORTED;
+    long long pairs = 0;
+    for (int a = 0; a < 4; a++) {
+        if (sections[a] < 0) return FB_ERR_SHAPE;
+        pairs += sections[a];
+    }
+    if (pairs < 1 || pairs > C / 2) return FB_ERR_SHAPE;
+    const int size = elem_size(dtype);
+    if (!aligned16(y0) || !aligned_to(x0, size) || !aligned_to(positions, 4) || !aligned_to(freqs, 4)) return FB_ERR_ALIGN;
+    if (H1 > 0 && (!aligned16(y1) || !aligned_to(x1, size))) return FB_ERR_ALIGN;
+    // in place: a row is read by the threads that write it, so only where it stays where it is
+    const auto contiguous = [&](const long long* s, int H) {
+        return (B == 1 || s[0] == (long long)H * N * C) && (H == 1 || s[1] == (long long)N * C) && (N == 1 || s[2] == C);
+    };
+    if (y0 == x0 && !contiguous(strides, H0)) return FB_ERR_UNSUPPORTED;
+    if (H1 > 0 && y1 == x1 && !contiguous(strides + 3, H1)) return FB_ERR_UNSUPPORTED;
+
+    RotaryParams p{};
+    p.t0 = {x0, y0, strides[0], strides[1], strides[2]};
+    if (H1 > 0) p.t1 = {x1, y1, strides[3], strides[4], strides[5]};
+    p.positions = positions; p.freqs = freqs;
+    p.B = B; p.N = N; p.C = C; p.H0 = H0; p.H1 = H1;
+    p.pairs = (int)pairs;
+    p.end0 = sections[0]; p.end1 = p.end0 + sections[1]; p.end2 = p.end1 + sections[2];
+    p.pos_f32 = positions_f32 != 0; p.pos_shared = positions_shared != 0; p.interleaved = interleaved != 0;
+    p.inverse = inverse;
+    const int rc = fb_launch_rotary(p, dtype == FB_F32, (hipStream_t)stream);
+    return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
+}
+
+int fb_rotary_fwd(const void* x0, void* y0, int H0, const void* x1, void* y1, int H1, const long long* strides,
+                  const void* positions, int positions_f32, int positions_shared, const float* freqs, const int* sections,
+                  int B, int N, int C, int interleaved, fb_dtype dtype, void* stream) {
+    return rotary_impl(x0, y0, H0, x1, y1, H1, strides, positions, positions_f32, positions_shared, freqs, sections, B, N, C,
+                       interleaved, dtype, 0, stream);
+}
+
+int fb_rotary_bwd(const void* dy0, void* dx0, int H0, const void* dy1, void* dx1, int H1, const long long* strides,
+                  const void* positions, int positions_f32, int positions_shared, const float* freqs, const int* sections,
+                  int B, int N, int C, int interleaved, fb_dtype dtype, void* stream) {
+    return rotary_impl(dy0, dx0, H0, dy1, dx1, H1, strides, positions, positions_f32, positions_shared, freqs, sections, B, N, C,
+                       interleaved, dtype, 1, stream);
+}
+
+// log2 of a page's rows, -1 for sizes that are not supported
+static int page_shift_of(int page) {
+    for (int s = 4; s <= 8; s++)
+        if (page == 1 << s) return s;
+    return -1;
+}
+
+// What the pages of a cache have to satisfy: slots and table entries are ints.
+static int check_pages(int page, int n_pages) {
+    if (n_pages <= 0) return FB_ERR_SHAPE;
+    const int shift = page_shift_of(page);
+    if (shift < 0) return FB_ERR_UNSUPPORTED;
+    return (long long)n_pages * page >= (1LL << 31) ? FB_ERR_SHAPE : FB_OK;
+}
+
+int fb_paged_plan(const int* lens, const int* new_lens, int* table, int* ring, const int* state,
+                  int* lens_out, int* state_out, int* slots, int* positions,
+                  int B, int N, int page, int n_pages, int max_blocks, void* stream) {
+    if (!lens || !new_lens || !table || !ring || !state || !lens_out || !state_out || !slots) return FB_ERR_NULL;
+    if (B <= 0 || N <= 0 || max_blocks <= 0) return FB_ERR_SHAPE;
+    if ((long long)B * N >= (1LL << 31) || (long long)B * max_blocks >= (1LL << 31)) return FB_ERR_SHAPE;
+    if (int st = check_pages(page, n_pages)) return st;
+    if (B > kFbPlanRequests) return FB_ERR_UNSUPPORTED;
+    const void* ptrs[] = {lens, new_lens, table, ring, state, lens_out, state_out, slots, positions};
+    for (const void* ptr : ptrs) if (!aligned_to(ptr, 4)) return FB_ERR_ALIGN;
+    // every workgroup reads all lengths and the state while others write the new ones
+    if (lens_out == lens || lens_out == new_lens || state_out == state) return FB_ERR_UNSUPPORTED;
+    PagedPlanParams p{};
+    p.lens = lens; p.new_lens = new_lens; p.table = table; p.ring = ring; p.state = state;
+    p.lens_out = lens_out; p.state_out = state_out; p.slots = slots; p.positions = positions;
+    p.B = B; p.N = N; p.page_shift = page_shift_of(page); p.n_pages = n_pages; p.max_blocks = max_blocks;
+    return fb_launch_paged_plan(p, (hipStream_t)stream) == 0 ? FB_OK : FB_ERR_LAUNCH;
+}
+
+int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* slots,
+                    void* k_pages, void* v_pages, void* phi_pages, const long long* strides,
+                    int B, int Hkv, int N, int C, int R, int page, int n_pages,
+                    fb_dtype dtype, fb_dtype phi_dtype, int phi_batch_broadcast, void* stream) {
+    if (!k || !v || !slots || !k_pages || !v_pages || !strides) return FB_ERR_NULL;
+    if (int st = check_common(B, Hkv, N, C, R)) return st;
+    if (R > 0 && (!phi_k || !phi_pages)) return FB_ERR_NULL;
+    if (int st = check_pages(page, n_pages)) return st;
+    if (!known(dtype) || (R > 0 && !known(phi_dtype)) || R > 64) return FB_ERR_UNSUPPORTED;
+    if (dtype == FB_F32 && R > 0 && phi_dtype != FB_F32) return FB_ERR_UNSUPPORTED;
+    const int size = elem_size(dtype);
+    if (!aligned_to(k, size) || !aligned_to(v, size) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned_to(slots, 4))
+        return FB_ERR_ALIGN;
+    if (R > 0 && (!aligned_to(phi_k, elem_size(phi_dtype)) || !aligned16(phi_pages))) return FB_ERR_ALIGN;
+    PagedAppendParams p{};
+    p.k = k; p.v = v;
+    p.k_sb = strides[0]; p.k_sh = strides[1]; p.k_sn = strides[2];
+    p.v_sb = strides[3]; p.v_sh = strides[4]; p.v_sn = strides[5];
+    p.phi_k = phi_k; p.phik_bstride = phi_batch_broadcast ? 0 : (long long)Hkv * N * R;
+    p.slots = slots; p.k_pages = k_pages; p.v_pages = v_pages; p.phi_pages = phi_pages;
+    p.B = B; p.Hkv = Hkv; p.N = N; p.C = C; p.R = R; p.page_shift = page_shift_of(page); p.n_pages = n_pages;
+    const int rc = fb_launch_paged_append(p, dtype == FB_F32, phi_dtype == FB_F32, (hipStream_t)stream);
+    return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
+}
+
+// Row tiles of a key head and the workgroups its call is split over; 0 workers for a shape that the call refuses.
+static int paged_workers(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype, int* row_tiles) {
+    *row_tiles = (int)(((long long)(H / Hkv) * N + 15) / 16);
+    return fb_paged_attn_workers(B, Hkv, *row_tiles, (long long)max_blocks * page, C, dtype == FB_F32);
+}
+
+size_t fb_paged_attn_fwd_workspace_bytes(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {
+    if (B <= 0 || H <= 0 || Hkv <= 0 || N <= 0 || max_blocks <= 0 || H % Hkv != 0) return 0;
+    if (check_common(B, H, N, C, 0) != FB_OK || page_shift_of(page) < 0 || !known(dtype)) return 0;
+    int row_tiles;
+    return fb_paged_attn_workspace_bytes(paged_workers(B, H, Hkv, N, C, page, max_blocks, dtype, &row_tiles), C);
+}
+
+int fb_paged_attn_fwd(const void* q, const void* k_pages, const void* v_pages,
+                      const void* phi_q, const void* phi_pages, const float* slopes,
+                      const int* table, const int* lens, const int* starts, void* out, float* lse,
+                      int B, int H, int Hkv, int N, int C, int R, int page, int n_pages, int max_blocks, int causal,
+                      fb_dtype dtype, fb_dtype phi_dtype, int phi_batch_broadcast, float scale,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !k_pages || !v_pages || !table || !lens || !out || !lse) return FB_ERR_NULL;
+    if (int st = check_common(B, H, N, C, R)) return st;
+    if (Hkv <= 0 || H % Hkv != 0 || max_blocks <= 0) return FB_ERR_SHAPE;
+    if ((long long)B * max_blocks >= (1LL << 31)) return FB_ERR_SHAPE;
+    if (R > 0 && (!phi_q || !phi_pages)) return FB_ERR_NULL;
+    if (int st = check_pages(page, n_pages)) return st;
+    if (!known(dtype) || (R > 0 && !known(phi_dtype)) || R > 64) return FB_ERR_UNSUPPORTED;
+    if (dtype == FB_F32 && R > 0 && phi_dtype != FB_F32) return FB_ERR_UNSUPPORTED;
+    if (slopes && R > 0) return FB_ERR_UNSUPPORTED;                  // one bias or the other
+    const void* ptrs[] = {q, k_pages, v_pages, out, lse, workspace};
+    for (const void* ptr : ptrs) if (!aligned16(ptr)) return FB_ERR_ALIGN;
+    if (R > 0 && (!aligned_to(phi_q, elem_size(phi_dtype)) || !aligned16(phi_pages))) return FB_ERR_ALIGN;
+    if (!aligned_to(slopes, 4) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(starts, 4)) return FB_ERR_ALIGN;
+
+    PagedAttnParams p{};
+    p.q = q; p.k_pages = k_pages; p.v_pages = v_pages; p.phi_q = phi_q; p.phi_pages = phi_pages; p.slopes = slopes;
+    p.table = table; p.lens = lens; p.starts = starts; p.out = out; p.lse = lse;
+    p.phiq_bstride = phi_batch_broadcast ? 0 : (long long)H * N * R;
+    p.B = B; p.H = H; p.Hkv = Hkv; p.N = N; p.R = R; p.page_shift = page_shift_of(page); p.n_pages = n_pages;
+    p.max_blocks = max_blocks; p.causal = causal != 0; p.phi_f32 = phi_dtype == FB_F32;
+    p.scale = scale > 0.f ? scale : 1.0f / std::sqrt((float)C);
+    p.workers = paged_workers(B, H, Hkv, N, C, page, max_blocks, dtype, &p.row_tiles);
+    // without room for the parts a key head stays in one workgroup
+    if (!workspace || workspace_bytes < fb_paged_attn_workspace_bytes(p.workers, C)) p.workers = 0;
+    const int rc = fb_launch_paged_attn(p, C, dtype == FB_F32, workspace, (hipStream_t)stream);
+    return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_UNSUPPORTED : FB_ERR_LAUNCH);
+}
+
 }  // extern "C"
 #pragma GCC visibility pop

@@ -57,6 +57,18 @@ int fb_launch_mulbias_fold(const void* x, const void* phi, const void* g_head, c
 int fb_launch_fold_batch(const void* s0, void* d0, long long n0, const void* s1, void* d1, long long n1, int B, bool f32,
                          hipStream_t stream);
 
+// Rotary positions.
+int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream);
+
+// Pages of a key-value cache: tables and slots from request lengths, storing of new rows, attention over the pages.
+constexpr int kFbPlanRequests = 4096;       // requests one plan takes
+int fb_launch_paged_plan(const PagedPlanParams& p, hipStream_t stream);
+int fb_launch_paged_append(PagedAppendParams p, bool f32, bool phi_f32, hipStream_t stream);
+// Workgroups that share the keys of a call whose requests have up to `capacity` keys each, 0: no split (no scratch).
+int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32);
+size_t fb_paged_attn_workspace_bytes(int workers, int C);
+int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream_t stream);
+
 // A kernel's dynamic-LDS limit is an attribute of the (kernel, device) pair: raise it on the
 // first launch on each device.  Racing first launches all set the same value; the flag is
 // published only after the attribute call has returned.

@@ -2,6 +2,7 @@
 #ifndef FB_PARAMS_H_
 #define FB_PARAMS_H_
 
+#include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -57,6 +58,76 @@ struct BwdParams {
     int n_tiles;          // tiles per (b,h) along the kernel's outer dimension
     int total_tiles;
     int tiles_per_xcd;
+};
+
+// Rotary positions: one tensor of rows [B, heads, N, C], read with strides (elements), written contiguously.
+struct RotaryTensor {
+    const void* x;
+    void* y;
+    long long sb, sh, sn;
+};
+
+struct RotaryParams {
+    RotaryTensor t0, t1;     // H1 = 0: the first only
+    const void* positions;   // [axes, B or 1, N] int or float
+    const float* freqs;      // [pairs]
+    int B, N, C, H0, H1;
+    int pairs;               // turned pairs of a row
+    int end0, end1, end2;    // pairs of the first axis, of the first two, of the first three
+    int pos_f32, pos_shared, interleaved;
+    int inverse;             // turn back (the backward)
+    int heads_per_group;     // set by the launch
+};
+
+// Pages of a key-value cache.  Requests b = 0..B-1 own ceil(len / page) pages each, table[b][0..).
+struct PagedPlanParams {
+    const int* lens;         // [B] tokens held
+    const int* new_lens;     // [B] tokens wanted
+    int* table;              // [B, max_blocks]
+    int* ring;               // [n_pages] free pages, count of them from head on
+    const int* state;        // head, count
+    int* lens_out;           // [B]
+    int* state_out;
+    int* slots;              // [B, N]
+    int* positions;          // [B, N] or null
+    int B, N, page_shift, n_pages, max_blocks;
+};
+
+struct PagedAppendParams {
+    const void* k;           // [B, Hkv, N, C] with strides
+    const void* v;
+    long long k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+    const void* phi_k;       // [Bp, Hkv, N, R] or null
+    long long phik_bstride;  // 0 when shared over the batch
+    const int* slots;        // [B, N]
+    void* k_pages;           // [n_pages, Hkv, page, C]
+    void* v_pages;
+    void* phi_pages;         // [n_pages, Hkv, page, R]
+    int B, Hkv, N, C, R, page_shift, n_pages;
+    int heads_per_group;     // set by the launch
+};
+
+struct PagedAttnParams {
+    const void* q;           // [B, H, N, C]
+    const void* k_pages;     // [n_pages, Hkv, page, C]
+    const void* v_pages;
+    const void* phi_q;       // [Bp, H, N, R] or null
+    const void* phi_pages;   // [n_pages, Hkv, page, R]
+    const float* slopes;     // [H] or null
+    const int* table;        // [B, max_blocks]
+    const int* lens;         // [B]
+    const int* starts;       // [B] position of a request's first query, or null: lens - N
+    void* out;               // [B, H, N, C]
+    float* lse;              // [B, H, N]
+    long long phiq_bstride;
+    int B, H, Hkv, N, R, page_shift, n_pages, max_blocks, causal, phi_f32;
+    float scale;
+    int row_tiles;           // query rows of a key head (H / Hkv * N of them) in tiles of 16
+    int workers;             // workgroups the keys are split over; 0: one per key head and row tile, no split
+    float* part_o;           // scratch: two parts per worker, [workers, 2, 16, C]
+    float* part_m;           // [workers, 2, 16] maxima
+    float* part_l;           // [workers, 2, 16] sums
+    int4* joins;             // [workers] what the join has to do behind this worker
 };
 
 #endif
