@@ -727,17 +727,24 @@ int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* 
     return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
 }
 
-// Row tiles of a key head and the workgroups its call is split over; 0 workers for a shape that the call refuses.
-static int paged_workers(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype, int* row_tiles) {
-    *row_tiles = (int)(((long long)(H / Hkv) * N + 15) / 16);
-    return fb_paged_attn_workers(B, Hkv, *row_tiles, (long long)max_blocks * page, C, dtype == FB_F32);
+// Row tiles of a key head, the waves a call is split over, and the scratch for them.
+struct PagedSplit {
+    int row_tiles, workers;
+    size_t bytes;
+};
+static PagedSplit paged_split(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {
+    const long long rows = (long long)(H / Hkv) * N;
+    PagedSplit s;
+    s.row_tiles = (int)((rows + 15) / 16);
+    s.workers = fb_paged_attn_workers(B, Hkv, s.row_tiles, (long long)max_blocks * page, C, dtype == FB_F32);
+    s.bytes = s.workers ? fb_paged_attn_workspace_bytes(s.workers, (long long)B * Hkv * s.row_tiles, rows, C) : 0;
+    return s;
 }
 
 size_t fb_paged_attn_fwd_workspace_bytes(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {
     if (B <= 0 || H <= 0 || Hkv <= 0 || N <= 0 || max_blocks <= 0 || H % Hkv != 0) return 0;
     if (check_common(B, H, N, C, 0) != FB_OK || page_shift_of(page) < 0 || !known(dtype)) return 0;
-    int row_tiles;
-    return fb_paged_attn_workspace_bytes(paged_workers(B, H, Hkv, N, C, page, max_blocks, dtype, &row_tiles), C);
+    return paged_split(B, H, Hkv, N, C, page, max_blocks, dtype).bytes;
 }
 
 int fb_paged_attn_fwd(const void* q, const void* k_pages, const void* v_pages,
@@ -767,9 +774,10 @@ int fb_paged_attn_fwd(const void* q, const void* k_pages, const void* v_pages,
     p.B = B; p.H = H; p.Hkv = Hkv; p.N = N; p.R = R; p.page_shift = page_shift_of(page); p.n_pages = n_pages;
     p.max_blocks = max_blocks; p.causal = causal != 0; p.phi_f32 = phi_dtype == FB_F32;
     p.scale = scale > 0.f ? scale : 1.0f / std::sqrt((float)C);
-    p.workers = paged_workers(B, H, Hkv, N, C, page, max_blocks, dtype, &p.row_tiles);
+    const PagedSplit split = paged_split(B, H, Hkv, N, C, page, max_blocks, dtype);
+    p.row_tiles = split.row_tiles;
     // without room for the parts a key head stays in one workgroup
-    if (!workspace || workspace_bytes < fb_paged_attn_workspace_bytes(p.workers, C)) p.workers = 0;
+    p.workers = workspace && workspace_bytes >= split.bytes ? split.workers : 0;
     const int rc = fb_launch_paged_attn(p, C, dtype == FB_F32, workspace, (hipStream_t)stream);
     return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_UNSUPPORTED : FB_ERR_LAUNCH);
 }

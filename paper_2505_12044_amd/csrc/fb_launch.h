@@ -64,9 +64,10 @@ int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream);
 constexpr int kFbPlanRequests = 4096;       // requests one plan takes
 int fb_launch_paged_plan(const PagedPlanParams& p, hipStream_t stream);
 int fb_launch_paged_append(PagedAppendParams p, bool f32, bool phi_f32, hipStream_t stream);
-// Workgroups that share the keys of a call whose requests have up to `capacity` keys each, 0: no split (no scratch).
+// Waves that share the keys of a call whose requests have up to `capacity` keys each, 0: no split (no scratch).
 int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32);
-size_t fb_paged_attn_workspace_bytes(int workers, int C);
+// groups: B * Hkv * row_tiles; rows: query rows of a key head
+size_t fb_paged_attn_workspace_bytes(int workers, long long groups, long long rows, int C);
 int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream_t stream);
 
 // A kernel's dynamic-LDS limit is an attribute of the (kernel, device) pair: raise it on the

@@ -13,10 +13,11 @@
 // rounding to one would be as large as that of the result); scores, maxima and sums are fp32, in natural units (a bias
 // of the type's lowest value keeps its differences).  fp32 tensors and all factors take the fp32 matrix instruction.
 //
-// The keys of all requests are laid end to end in steps of 4 KW keys, and each of `workers` workgroups takes an equal
-// share, found from the lengths on the device: one long request among short ones, or a table with room for far more
-// than it holds, costs no balance.  A share ends inside a (request, key head): the parts go to scratch, two per
-// worker at most, and a second launch joins them in a fixed order.
+// The keys of all (request, key head, row tile) groups are laid end to end in steps of KW keys, and each of `workers`
+// waves takes an equal share, found from the lengths on the device: one long request among short ones, or a table with
+// room for far more than it holds, costs no balance, and no wave waits for another.  A share may end inside a group: the
+// parts go to scratch, two per worker at most, and a second launch joins them in a fixed order.  Without scratch, and
+// where no request can be long, a workgroup's four waves share one group and join through LDS.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -30,17 +31,26 @@ namespace {
 constexpr int kPaWaves = 4;
 constexpr int kPaThreads = kPaWaves * 64;
 constexpr int kPaRows = 16;
-constexpr int kPaLeast = 2;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
+constexpr int kPaLeast = 4;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-FB_DEV float lane_xor_max(float x) {      // over the four lanes of a column
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return half_max(x);
+// Both values of the rows of 16 lanes 2 n, 2 n + 1 in both rows (half_pair of fb_device.h, one level down).
+FB_DEV HalfPair row_pair(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    unsigned w = u;
+    asm volatile("" : "+v"(w));
+    auto r = __builtin_amdgcn_permlane16_swap(u, w, false, false);
+    return {__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])};
 }
-FB_DEV float lane_xor_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return half_sum(x);
+// over the four lanes of a column
+FB_DEV float column_max(float x) {
+    const HalfPair p = row_pair(x);
+    return half_max(fmaxf(p.lo, p.hi));
+}
+FB_DEV float column_sum(float x) {
+    const HalfPair p = row_pair(x);
+    return half_sum(p.lo + p.hi);
 }
 
 // exp(a - m) for a <= m; 0 where a is -inf, whatever m is
@@ -153,106 +163,227 @@ struct Step<float, C> {
 
 enum { kBiasNone = 0, kBiasAlibi = 1, kBiasFactors4 = 2, kBiasFactors = 3 };    // factors: up to 4, any number
 
-// Sums over the workgroup; every thread gets the total and its own inclusive sum.
-FB_DEV long long pa_scan(long long x, long long* sm, long long& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Arrays that are not written while the kernel runs, read at wave-uniform places: scalar loads, which do not queue behind
+// the rows in flight.
+typedef const __attribute__((address_space(4))) int* ConstInts;
+FB_DEV ConstInts const_ints(const int* x) { return (ConstInts)(uintptr_t)x; }
+
+FB_DEV int held_keys(const PagedAttnParams& p, int b) {
+    return max((int)min((long long)const_ints(p.lens)[b], (long long)p.max_blocks << p.page_shift), 0);
+}
+
+// Steps of a request per group; one that holds nothing has one too (its rows are written).
+template <int KW>
+FB_DEV int steps_of(int len) { return len > KW ? (len + KW - 1) / KW : 1; }
+
+// Inclusive sums over the wave.
+FB_DEV long long wave_scan(long long x) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const long long y = __shfl_up(x, d);
         if (lane >= d) x += y;
     }
-    if (lane == 63) sm[wave] = x;
-    __syncthreads();
-    long long before = 0;
-    total = 0;
+    return x;
+}
+
+// The steps of all requests laid end to end, cut in equal shares: where this wave's begins and ends.  `total`, `workers`
+// (those that have a share), `u`, `u_end`: steps; b, rem: the request that step u lies in and its place there.
+struct Share {
+    long long total, u, u_end, rem;
+    int workers, b;
+};
+
+template <int KW>
+FB_DEV Share share_of(const PagedAttnParams& p, int groups, int worker) {
+    __shared__ long long sm_sum[kPaWaves];
+    __shared__ long long sm_rem[kPaWaves];
+    __shared__ int sm_b[kPaWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Share s{};
+    const auto cut = [&]() {
+        s.workers = (int)min((long long)p.workers, (s.total + kPaLeast - 1) / kPaLeast);
+        s.u = worker * s.total / s.workers;
+        s.u_end = worker < s.workers ? (worker + 1) * s.total / s.workers : s.u;
+    };
+    if (p.B <= 64) {                                     // every wave by itself
+        const long long own = lane < p.B ? (long long)steps_of<KW>(max((int)min((long long)p.lens[lane], (long long)p.max_blocks << p.page_shift), 0)) * groups : 0;
+        const long long end = wave_scan(own);
+        s.total = __shfl(end, 63);
+        cut();
+        if (s.u < s.u_end) {
+            s.b = __builtin_ctzll(__ballot(end > s.u));
+            s.rem = s.u - __shfl(end - own, s.b);
+        }
+        return s;
+    }
+    // the workgroup's four shares together, 256 requests at a time: the total first
+    const auto tile = [&](int b0, long long& own, long long& sum) {
+        const int b = b0 + tid;
+        own = b < p.B ? (long long)steps_of<KW>(max((int)min((long long)p.lens[b], (long long)p.max_blocks << p.page_shift), 0)) * groups : 0;
+        const long long in_wave = wave_scan(own);
+        __syncthreads();
+        if (lane == 63) sm_sum[wave] = in_wave;
+        __syncthreads();
+        long long before = 0;
+        sum = 0;
 #pragma unroll
-    for (int w = 0; w < kPaWaves; w++) {
-        if (w < wave) before += sm[w];
-        total += sm[w];
+        for (int w = 0; w < kPaWaves; w++) {
+            if (w < wave) before += sm_sum[w];
+            sum += sm_sum[w];
+        }
+        return before + in_wave;
+    };
+    long long own, sum;
+    for (int b0 = 0; b0 < p.B; b0 += kPaThreads) {
+        tile(b0, own, sum);
+        s.total += sum;
+    }
+    cut();
+    long long before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kPaThreads) {
+        const long long end = before + tile(b0, own, sum);
+        for (int w = 0; w < kPaWaves; w++) {
+            const int k = worker - wave + w;
+            const long long u = k * s.total / s.workers;
+            if (end - own <= u && u < end) {
+                sm_b[w] = b0 + tid;
+                sm_rem[w] = u - (end - own);
+            }
+        }
+        before += sum;
     }
     __syncthreads();
-    return x + before;
+    s.b = sm_b[wave];                                    // (waves without a share do not read on)
+    s.rem = sm_rem[wave];
+    return s;
 }
 
-FB_DEV int held_keys(const PagedAttnParams& p, int b) {
-    return max((int)min((long long)p.lens[b], (long long)p.max_blocks << p.page_shift), 0);
+// Four channels of a result row from its sums.
+template <typename T, int C>
+FB_DEV void write_row(const PagedAttnParams& p, long long row, int c4, const f32x4& o, float l, float m) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    struct alignas(4 * sizeof(T)) Four { T x[4]; } v;
+#pragma unroll
+    for (int e = 0; e < 4; e++) v.x[e] = (T)(l == 0.f ? 0.f : o[e] * inv);
+    *(Four*)((T*)p.out + row * C + c4 * 4) = v;
+    if (c4 == 0) p.lse[row] = l == 0.f ? -INFINITY : m + __log2f(l) * kLn2;
 }
+
+// One wave's (SPLIT) or workgroup's part of a group: steps t0..t1 of n_steps.
+struct Segment {
+    int b, len, n_steps, grp, t0, t1;
+};
 
 // BIAS, PF32: kind of bias and whether the factors are float
-template <typename T, int C, int BIAS, bool PF32>
+template <typename T, int C, int BIAS, bool PF32, bool SPLIT>
 __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnParams p) {
     using S = Step<T, C>;
-    constexpr int KW = S::KW, TK = kPaWaves * KW, NV = S::NV, GROUPS = S::GROUPS;
-    constexpr int OP = C + 4;                             // LDS row pitch: 16 rows of a wave's O start in different banks
+    constexpr int KW = S::KW, NV = S::NV, GROUPS = S::GROUPS;
+    constexpr int STRIDE = SPLIT ? KW : kPaWaves * KW;    // keys from one step of a wave to its next
+    constexpr int NF = BIAS == kBiasFactors4 ? 1 : (BIAS == kBiasFactors ? 4 : 0);
     using PT = std::conditional_t<PF32, float, bf16_t>;
-    __shared__ __align__(16) float sm_o[kPaWaves][kPaRows][OP];
-    __shared__ float sm_m[kPaWaves][kPaRows], sm_l[kPaWaves][kPaRows];
-    __shared__ long long sm_scan[kPaWaves];
-    __shared__ long long sm_at[2];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, i = lane & 15;
-    const int groups = p.Hkv * p.row_tiles;               // (key head, row tile) pairs of a request
+    const int groups = p.Hkv * p.row_tiles;               // of a request
     const int rows_all = p.H / p.Hkv * p.N;
+    const int part_rows = min(kPaRows, rows_all);
     const int page_mask = (1 << p.page_shift) - 1;
 
-    auto steps_of = [&](int len) { return len > TK ? (len + TK - 1) / TK : 1; };      // a request without keys has one step too
-
-    // ---- this worker's share: steps [u, u_end) of all, the first of them in request b, `rem` steps into it ----
-    int b;
-    long long u, u_end, rem, total = 0, n_workers = 0;
-    if (p.workers == 0) {
-        b = blockIdx.x / groups;
-        const int len = held_keys(p, b);
-        rem = (long long)(blockIdx.x - b * groups) * steps_of(len);
-        u = 0;
-        u_end = steps_of(len);
-    } else {
-        for (int b0 = 0; b0 < p.B; b0 += kPaThreads) {
-            const int bb = b0 + tid;
-            long long sum;
-            pa_scan(bb < p.B ? (long long)steps_of(held_keys(p, bb)) * groups : 0, sm_scan, sum);
-            total += sum;
-        }
-        n_workers = min((long long)p.workers, (total + kPaLeast - 1) / kPaLeast);
-        const int w = blockIdx.x;
-        if (w >= n_workers) {
-            if (tid == 0) p.joins[w] = make_int4(0, 0, 0, 0);
+    Segment seg;
+    Share share{};
+    const int worker = blockIdx.x * kPaWaves + wave;
+    long long left = 0;                                   // steps of this worker behind the segment
+    if constexpr (SPLIT) {
+        share = share_of<KW>(p, groups, worker);
+        if (share.u >= share.u_end) {
+            if (!p.joins_by_group && worker < p.workers && lane == 0) p.joins[worker] = make_int4(0, 0, 0, 0);
             return;
         }
-        u = w * total / n_workers;
-        u_end = (w + 1) * total / n_workers;
-        long long before = 0;
-        for (int b0 = 0; b0 < p.B; b0 += kPaThreads) {
-            const int bb = b0 + tid;
-            const long long own = bb < p.B ? (long long)steps_of(held_keys(p, bb)) * groups : 0;
-            long long sum;
-            const long long end = before + pa_scan(own, sm_scan, sum);
-            if (end - own <= u && u < end) {
-                sm_at[0] = bb;
-                sm_at[1] = u - (end - own);
-            }
-            before += sum;
-            if (before > u) break;                        // (uniform)
-        }
-        __syncthreads();
-        b = (int)sm_at[0];
-        rem = sm_at[1];
+        seg.b = __builtin_amdgcn_readfirstlane(share.b);
+        seg.len = held_keys(p, seg.b);
+        seg.n_steps = steps_of<KW>(seg.len);
+        const unsigned rem = __builtin_amdgcn_readfirstlane((int)share.rem);      // < groups * steps of one request < 2^31
+        seg.grp = (int)(rem / (unsigned)seg.n_steps);
+        seg.t0 = (int)rem - seg.grp * seg.n_steps;
+        left = share.u_end - share.u;
+        left = ((long long)__builtin_amdgcn_readfirstlane((int)(left >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)left);
+        seg.t1 = (int)min((long long)seg.n_steps, seg.t0 + left);
+        left -= seg.t1 - seg.t0;
+    } else {
+        seg.b = blockIdx.x / groups;
+        seg.grp = blockIdx.x - seg.b * groups;
+        seg.len = held_keys(p, seg.b);
+        seg.t0 = 0;
+        seg.t1 = seg.n_steps = steps_of<KW>(seg.len);
     }
-    b = __builtin_amdgcn_readfirstlane(b);
     int4 join = make_int4(0, 0, 0, 0);
 
-    while (u < u_end) {
-        const int len = __builtin_amdgcn_readfirstlane(held_keys(p, b));
-        const int n_steps = steps_of(len);
-        const int grp = __builtin_amdgcn_readfirstlane((int)(rem / n_steps));
-        const int t0 = __builtin_amdgcn_readfirstlane((int)(rem - (long long)grp * n_steps));
-        const int t1 = __builtin_amdgcn_readfirstlane((int)min((long long)n_steps, t0 + (u_end - u)));
-        const int h = grp / p.row_tiles, r0 = (grp - h * p.row_tiles) * kPaRows;
-        const int rows = min(kPaRows, rows_all - r0);
-        const int start = __builtin_amdgcn_readfirstlane(p.starts ? min(max(p.starts[b], -(1 << 30)), 1 << 30) : len - p.N);
-        const long long row_base = (long long)b * p.H * p.N + (long long)h * rows_all + r0;      // of q, out, lse
+    // ---- what a step reads ----
+    // pages of the 16-key groups from key k on (-1 behind `end`), and the first row of each in its page; a group whose page is
+    // none is not visible, and the first rows of page 0 stand in for it
+    auto pages_at = [&](int (&page)[GROUPS], const Segment& s, int k, int end) __attribute__((always_inline)) {
+        const ConstInts table = const_ints(p.table) + (long long)s.b * p.max_blocks;
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) page[x] = k + 16 * x < end ? table[(k + 16 * x) >> p.page_shift] : -1;
+    };
+    auto rows_of = [&](long long (&row)[GROUPS], const int (&page)[GROUPS], int h, int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++)
+            row[x] = (unsigned)page[x] < (unsigned)p.n_pages
+                         ? (((long long)page[x] * p.Hkv + h) << p.page_shift) + ((k + 16 * x) & page_mask) : -1;
+    };
+    typename S::Keys kr;
+    typename S::Values vr;
+    PT fr[GROUPS][NF > 0 ? NF : 1];
+    // Factors of one row, the lane's share: factor g (up to four), or 4 g .. 4 g + 3 of the first 16, at once where rows allow.
+    const bool factors_x4 = NF == 4 && p.R % 4 == 0;
+    auto load_factors = [&](PT (&f)[NF > 0 ? NF : 1], const PT* pk) __attribute__((always_inline)) {
+        if (factors_x4) {
+            struct alignas(4 * sizeof(PT)) Four { PT x[4]; } v = {};
+            if (4 * g < p.R) v = *(const Four*)(pk + 4 * g);
+#pragma unroll
+            for (int y = 0; y < NF; y++) f[y] = v.x[y];
+        } else {
+#pragma unroll
+            for (int y = 0; y < NF; y++) f[y] = NF * g + y < p.R ? pk[NF * g + y] : (PT)0.f;
+        }
+    };
+    auto load_keys = [&](const long long (&row)[GROUPS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) {
+            const long long at = row[x] >= 0 ? row[x] : 0;
+            S::load_keys(kr, x, (const T*)p.k_pages + at * C, g, i);
+            if constexpr (NF > 0) {
+                load_factors(fr[x], (const PT*)p.phi_pages + (at + i) * p.R);
+            }
+        }
+    };
+    auto load_values = [&](const long long (&row)[GROUPS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) S::load_values(vr, x, (const T*)p.v_pages + (row[x] >= 0 ? row[x] : 0) * C, g, i);
+    };
+    auto first_key = [&](const Segment& s) { return s.t0 * KW + (SPLIT ? 0 : wave * KW); };
+    auto key_end = [&](const Segment& s) { return min(s.len, s.t1 * KW); };
+
+    // One step ahead: the next keys are loaded when the scores have used this step's, the next values after this step's
+    // product; the next segment's first step counts as the last step's next.  Pages are read a step before that.
+    long long row[GROUPS], next[GROUPS];
+    int page[GROUPS];
+    pages_at(page, seg, first_key(seg), key_end(seg));
+    rows_of(row, page, seg.grp / p.row_tiles, first_key(seg));
+    if (first_key(seg) < key_end(seg)) {
+        load_keys(row);
+        load_values(row);
+    }
+
+    for (;;) {
+        const int h = seg.grp / p.row_tiles, r0 = (seg.grp - h * p.row_tiles) * kPaRows;
+        const int rows = min(kPaRows, rows_all - r0), len = seg.len;
+        const int start = p.starts ? min(max(const_ints(p.starts)[seg.b], -(1 << 30)), 1 << 30) : len - p.N;
+        const long long row_base = (long long)seg.b * p.H * p.N + (long long)h * rows_all + r0;      // of q, out, lse
 
         // the lane's query row
         const bool has_row = i < rows;
@@ -265,71 +396,80 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
             q.x[x] = {};
             if (has_row) q.x[x] = S::row_chunk((const T*)p.q + (row_base + i) * C, g, x);
         }
-        float phi_q[4] = {0.f, 0.f, 0.f, 0.f};            // BIAS 2: [0] only; lane: factor 4 x + g
+        float phi_q[4] = {0.f, 0.f, 0.f, 0.f};
         const PT* pq_row = nullptr;
-        if constexpr (BIAS >= kBiasFactors4) {
-            pq_row = (const PT*)p.phi_q + (long long)b * p.phiq_bstride + ((long long)h * rows_all + r0 + i) * p.R;
-            constexpr int NF = BIAS == kBiasFactors4 ? 1 : 4;
+        if constexpr (NF > 0) {
+            pq_row = (const PT*)p.phi_q + (long long)seg.b * p.phiq_bstride + ((long long)h * rows_all + r0 + i) * p.R;
 #pragma unroll
             for (int x = 0; x < NF; x++)
-                if (has_row && 4 * x + g < p.R) phi_q[x] = (float)pq_row[4 * x + g];
+                if (has_row && NF * g + x < p.R) phi_q[x] = (float)pq_row[NF * g + x];
         }
         float slope = 0.f;
         if constexpr (BIAS == kBiasAlibi)
             if (has_row) slope = p.slopes[h * (p.H / p.Hkv) + (r0 + i) / p.N];
 
-        const int* table = p.table + (long long)b * p.max_blocks;
+        Segment after = seg;                              // the worker's next segment
+        const bool has_after = SPLIT && left > 0;
+        if constexpr (SPLIT) {
+            if (has_after) {
+                after.grp++;
+                if (after.grp == groups) {
+                    after.grp = 0;
+                    after.b++;
+                    after.len = held_keys(p, after.b);
+                    after.n_steps = steps_of<KW>(after.len);
+                }
+                after.t0 = 0;
+                after.t1 = (int)min((long long)after.n_steps, left);
+                left -= after.t1;
+            }
+        }
+
         float m = -INFINITY, l = 0.f;
         f32x4 o[NV];
 #pragma unroll
         for (int t = 0; t < NV; t++) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        // first row of the 16 keys from k on in their page, -1: no such page (its keys are not visible)
-        auto group_row = [&](int k) -> long long {
-            if (k >= len) return -1;
-            const int page = __builtin_amdgcn_readfirstlane(table[k >> p.page_shift]);
-            if ((unsigned)page >= (unsigned)p.n_pages) return -1;
-            return (((long long)page * p.Hkv + h) << p.page_shift) + (k & page_mask);
+        const int k_end = key_end(seg);
+        int k0 = first_key(seg);                          // wave-uniform
+        const auto next_pages = [&](int k) __attribute__((always_inline)) {       // of the step behind the one at k - STRIDE
+            if (k < k_end) pages_at(page, seg, k, k_end);
+            else if (has_after) pages_at(page, after, first_key(after), key_end(after));
         };
-
-        for (int t = t0; t < t1; t++) {
-            const int k0 = t * TK + wave * KW;            // wave-uniform
-            if (k0 >= len) break;
-            typename S::Keys kr;
-            typename S::Values vr;
-            long long row[GROUPS];
+        const bool idle = k0 >= k_end;                    // no keys at all: the next segment's first step is still to be loaded
+        next_pages(k0 + STRIDE);
+        if (idle && has_after) {
+            rows_of(row, page, after.grp / p.row_tiles, 0);
+            if (key_end(after) > 0) {
+                load_keys(row);
+                load_values(row);
+            }
+        }
+        for (; k0 < k_end; k0 += STRIDE) {
+            const bool more = k0 + STRIDE < k_end, load = more || (has_after && key_end(after) > 0);
+            if (more) rows_of(next, page, h, k0 + STRIDE);
+            else rows_of(next, page, after.grp / p.row_tiles, first_key(after));
+            if (more) next_pages(k0 + 2 * STRIDE);
             bool whole = k0 + KW <= all_see;
 #pragma unroll
-            for (int s = 0; s < GROUPS; s++) {
-                row[s] = group_row(k0 + 16 * s);
-                whole = whole && row[s] >= 0;
-            }
-#pragma unroll
-            for (int s = 0; s < GROUPS; s++) {
-                const long long at = row[s] >= 0 ? row[s] : 0;       // page 0 stands in
-                S::load_keys(kr, s, (const T*)p.k_pages + at * C, g, i);
-                S::load_values(vr, s, (const T*)p.v_pages + at * C, g, i);
-            }
+            for (int s = 0; s < GROUPS; s++) whole = whole && row[s] >= 0;
             f32x4 sc[GROUPS];
 #pragma unroll
             for (int s = 0; s < GROUPS; s++) {
                 sc[s] = S::scores(kr, s, q);
                 const int key0 = k0 + 16 * s + 4 * g;
-                if constexpr (BIAS >= kBiasFactors4) {
-                    const PT* pk = (const PT*)p.phi_pages + ((row[s] >= 0 ? row[s] : 0) + i) * p.R;
+                if constexpr (NF > 0) {
                     f32x4 f = {0.f, 0.f, 0.f, 0.f};
-                    constexpr int NF = BIAS == kBiasFactors4 ? 1 : 4;
 #pragma unroll
-                    for (int x = 0; x < NF; x++) {
-                        const float a = 4 * x + g < p.R ? (float)pk[4 * x + g] : 0.f;
-                        f = __builtin_amdgcn_mfma_f32_16x16x4f32(a, phi_q[x], f, 0, 0, 0);
-                    }
-                    if constexpr (BIAS == kBiasFactors)
+                    for (int x = 0; x < NF; x++) f = __builtin_amdgcn_mfma_f32_16x16x4f32((float)fr[s][x], phi_q[x], f, 0, 0, 0);
+                    if constexpr (BIAS == kBiasFactors) {
+                        const PT* pk = (const PT*)p.phi_pages + ((row[s] >= 0 ? row[s] : 0) + i) * p.R;
                         for (int x = 4; 4 * x < p.R; x++) {
                             const bool in = 4 * x + g < p.R;
                             const float a = in ? (float)pk[4 * x + g] : 0.f, c = in && has_row ? (float)pq_row[4 * x + g] : 0.f;
                             f = __builtin_amdgcn_mfma_f32_16x16x4f32(a, c, f, 0, 0, 0);
                         }
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; r++) sc[s][r] = fmaf(sc[s][r], p.scale, f[r]);
                 } else {
@@ -345,20 +485,21 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
                         if (key0 + r >= limit || row[s] < 0) sc[s][r] = -INFINITY;
                 }
             }
+            if (load) load_keys(next);
             // ---- softmax of the rows ----
             float mx = m;
 #pragma unroll
             for (int s = 0; s < GROUPS; s++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[s][r]);
-            mx = lane_xor_max(mx);
+            mx = column_max(mx);
             if (__any(mx > m)) {
                 const float alpha = weight(m, mx);
                 l *= alpha;
 #pragma unroll
-                for (int t2 = 0; t2 < NV; t2++)
+                for (int t = 0; t < NV; t++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) o[t2][r] *= alpha;
+                    for (int r = 0; r < 4; r++) o[t][r] *= alpha;
                 m = mx;
             }
             const float ref = m == -INFINITY ? 0.f : m;
@@ -373,159 +514,208 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
             // ---- values ----
             if (whole) {
 #pragma unroll
-                for (int t2 = 0; t2 < NV; t2++) o[t2] = S::product(vr, t2, pr, o[t2]);
+                for (int t = 0; t < NV; t++) o[t] = S::product(vr, t, pr, o[t]);
             } else {
                 // Values a row does not see may be anything (0 * inf is NaN), so rows of different limits are done one
                 // after the other with the values behind their limit cleared; at most N of them, only around the last keys.
-                auto masked = [&](int seen, bool mine) __attribute__((always_inline)) {
+                unsigned long long todo = __ballot(limit > k0);
+                while (todo != 0) {
+                    const int cut = min(__builtin_amdgcn_readlane(limit, __builtin_ctzll(todo)), k0 + KW);
+                    const bool mine = min(limit, k0 + KW) == cut;
                     typename S::Values vm = vr;
 #pragma unroll
                     for (int s = 0; s < GROUPS; s++)
 #pragma unroll
                         for (int r = 0; r < 4; r++)
-                            if (k0 + 16 * s + 4 * g + r >= seen || row[s] < 0) vm.x[s][r] = {};
+                            if (k0 + 16 * s + 4 * g + r >= cut || row[s] < 0) vm.x[s][r] = {};
 #pragma unroll
-                    for (int t2 = 0; t2 < NV; t2++) {
-                        const f32x4 d = S::product(vm, t2, pr, o[t2]);
+                    for (int t = 0; t < NV; t++) {
+                        const f32x4 d = S::product(vm, t, pr, o[t]);
 #pragma unroll
-                        for (int r = 0; r < 4; r++) o[t2][r] = mine ? d[r] : o[t2][r];
+                        for (int r = 0; r < 4; r++) o[t][r] = mine ? d[r] : o[t][r];
                     }
-                };
-                unsigned long long todo = __ballot(limit > k0);
-                while (todo != 0) {
-                    const int seen = __builtin_amdgcn_readlane(limit, __builtin_ctzll(todo));
-                    const int cut = min(seen, k0 + KW);
-                    const bool mine = min(limit, k0 + KW) == cut;
-                    masked(cut, mine);
                     todo &= ~__ballot(mine);
                 }
             }
+            if (load) load_values(next);
+#pragma unroll
+            for (int s = 0; s < GROUPS; s++) row[s] = next[s];
         }
 
-        // ---- the waves of the workgroup ----
-        l = lane_xor_sum(l);
-        __syncthreads();                                  // the last segment's sums have been read
-        if (has_row) {
-#pragma unroll
-            for (int r = 0; r < 4; r++)
-#pragma unroll
-                for (int t = 0; t < NV; t++) sm_o[wave][i][(4 * g + r) * NV + t] = o[t][r];
-            if (g == 0) {
-                sm_m[wave][i] = limit > 0 ? m : -INFINITY;       // a row that sees nothing went along with the others
-                sm_l[wave][i] = limit > 0 ? l : 0.f;
-            }
+        l = column_sum(l);
+        if (limit <= 0) {                                 // a row that sees nothing went along with the others
+            m = -INFINITY;
+            l = 0.f;
         }
-        __syncthreads();
-        const bool split = t0 > 0 || t1 < n_steps;
-        const int slot = blockIdx.x * 2 + (t0 > 0 ? 0 : 1);
-        for (int x = tid; x < rows * (C / 4); x += kPaThreads) {
-            const int r = x / (C / 4), c4 = x % (C / 4);
-            float mx = sm_m[0][r];
+        if constexpr (SPLIT) {
+            // The lane's channels of row i: 4 NV adjacent ones from 4 g NV on.
+            if (seg.t0 == 0 && seg.t1 == seg.n_steps) {
+                if (has_row) {
+                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    struct alignas(4 * NV * sizeof(T) < 16 ? 4 * NV * sizeof(T) : 16) Mine { T x[4 * NV]; } v;
 #pragma unroll
-            for (int w = 1; w < kPaWaves; w++) mx = fmaxf(mx, sm_m[w][r]);
-            float lt = 0.f;
-            f32x4 ot = {0.f, 0.f, 0.f, 0.f};
+                    for (int r = 0; r < 4; r++)
 #pragma unroll
-            for (int w = 0; w < kPaWaves; w++) {
-                const float a = weight(sm_m[w][r], mx);
-                const f32x4 y = *(const f32x4*)&sm_o[w][r][c4 * 4];
-                lt = fmaf(a, sm_l[w][r], lt);
+                        for (int t = 0; t < NV; t++) v.x[r * NV + t] = (T)(l == 0.f ? 0.f : o[t][r] * inv);
+                    *(Mine*)((T*)p.out + (row_base + i) * C + 4 * g * NV) = v;
+                    if (g == 0) p.lse[row_base + i] = l == 0.f ? -INFINITY : m + __log2f(l) * kLn2;
+                }
+            } else if (has_row) {
+                const long long at = ((long long)worker * 2 + (seg.t0 > 0 ? 0 : 1)) * part_rows + i;
+                struct alignas(16) Mine { float x[4 * NV]; } v;
 #pragma unroll
-                for (int e = 0; e < 4; e++) ot[e] = fmaf(a, y[e], ot[e]);
-            }
-            if (!split) {
-                const float inv = lt == 0.f ? 0.f : 1.f / lt;
-                T* out = (T*)p.out + (row_base + r) * C + c4 * 4;
-                struct alignas(4 * sizeof(T)) Four { T x[4]; } v;
+                for (int r = 0; r < 4; r++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) v.x[e] = (T)(lt == 0.f ? 0.f : ot[e] * inv);
-                *(Four*)out = v;
-                if (c4 == 0) p.lse[row_base + r] = lt == 0.f ? -INFINITY : mx + __log2f(lt) * kLn2;
-            } else {
-                const long long at = (long long)slot * kPaRows + r;
-                *(f32x4*)(p.part_o + at * C + c4 * 4) = ot;
-                if (c4 == 0) {
-                    p.part_m[at] = mx;
-                    p.part_l[at] = lt;
+                    for (int t = 0; t < NV; t++) v.x[r * NV + t] = o[t][r];
+                *(Mine*)(p.part_o + at * C + 4 * g * NV) = v;
+                if (g == 0) {
+                    p.part_m[at] = m;
+                    p.part_l[at] = l;
                 }
             }
-        }
-        if (t0 == 0 && t1 < n_steps) {                    // the first of several workers
-            const long long last = u + n_steps - 1;       // the group's last step, and who has it
-            const long long lw = ((last + 1) * n_workers - 1) / total;
-            join = make_int4((int)(lw - blockIdx.x), (int)(row_base & 0xffffffff), (int)(row_base >> 32), rows);
-        }
-        u += t1 - t0;
-        rem += t1 - t0;
-        if (rem == (long long)groups * n_steps) {
-            b++;
-            rem = 0;
+            if (seg.t0 == 0) {                            // the group's first worker says who has the rest
+                int more = 0;
+                if (seg.t1 < seg.n_steps) {
+                    // the group's last step is share.u_end - 1 + (n_steps - t1): here the share ends inside the group
+                    const long long last = share.u_end - 1 + (seg.n_steps - seg.t1);
+                    more = (int)(((last + 1) * share.workers - 1) / share.total) - worker;
+                }
+                const int4 mine = make_int4(more, worker, (int)((long long)seg.b * groups + seg.grp), rows);
+                if (p.joins_by_group) {
+                    if (lane == 0) p.joins[mine.z] = mine;
+                } else if (more > 0) {
+                    join = mine;
+                }
+            }
+            if (!has_after) break;
+            seg = after;
+        } else {
+            // ---- the waves of the workgroup ----
+            __shared__ __align__(16) float sm_o[kPaWaves][kPaRows][C + 4];      // + 4: rows start in different banks
+            __shared__ float sm_m[kPaWaves][kPaRows], sm_l[kPaWaves][kPaRows];
+            if (has_row) {
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+#pragma unroll
+                    for (int t = 0; t < NV; t++) sm_o[wave][i][(4 * g + r) * NV + t] = o[t][r];
+                if (g == 0) {
+                    sm_m[wave][i] = m;
+                    sm_l[wave][i] = l;
+                }
+            }
+            __syncthreads();
+            for (int x = tid; x < rows * (C / 4); x += kPaThreads) {
+                const int r = x / (C / 4), c4 = x % (C / 4);
+                float mx = sm_m[0][r];
+#pragma unroll
+                for (int w = 1; w < kPaWaves; w++) mx = fmaxf(mx, sm_m[w][r]);
+                float lt = 0.f;
+                f32x4 ot = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kPaWaves; w++) {
+                    const float a = weight(sm_m[w][r], mx);
+                    const f32x4 y = *(const f32x4*)&sm_o[w][r][c4 * 4];
+                    lt = fmaf(a, sm_l[w][r], lt);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) ot[e] = fmaf(a, y[e], ot[e]);
+                }
+                write_row<T, C>(p, row_base + r, c4, ot, lt, mx);
+            }
+            break;
         }
     }
-    if (p.workers != 0 && tid == 0) p.joins[blockIdx.x] = join;
+    if constexpr (SPLIT)
+        if (!p.joins_by_group && lane == 0) p.joins[worker] = join;
 }
 
-// Joins the parts of one row: part 1 of the worker where the group begins and part 0 of the `more` workers behind it.
+// Joins the parts of a group's rows: part 1 of the worker where the group begins and part 0 of the `more` workers behind
+// it.  A workgroup takes `8 / lanes` rows of one group, `lanes` parts at a time.
 template <typename T, int C>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
-    constexpr int LN = C / 4, PL = 256 / LN;              // lanes of a row, parts at a time
-    __shared__ __align__(16) float sm_o[PL][C];
-    __shared__ float sm_l[PL], sm_m[4];
+__global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, int lanes) {
+    constexpr int LN = C / 4, SL = 8;                     // threads of a row, (row, part) slots
+    __shared__ __align__(16) float sm_o[SL][C];
+    __shared__ float sm_l[SL];
     const int4 join = p.joins[blockIdx.x];
-    const int more = join.x, r = blockIdx.y;
-    if (more == 0 || r >= join.w) return;
-    const long long row = (((long long)join.z << 32) | (unsigned)join.y) + r;
-    const int tid = threadIdx.x, c4 = tid % LN, pl = tid / LN;
-    auto part = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * kPaRows + r; };
+    const int more = join.x, first = join.y;
+    const int tid = threadIdx.x, c4 = tid % LN, slot = tid / LN, lane = slot % lanes;
+    const int r = blockIdx.y * (SL / lanes) + slot / lanes;
+    if (more == 0) return;                                // (uniform)
+    const bool has_row = r < join.w;
+    const int part_rows = min(kPaRows, p.H / p.Hkv * p.N);
+    auto part = [&](int k) { return ((long long)(first + k) * 2 + (k == 0 ? 1 : 0)) * part_rows + (has_row ? r : 0); };
 
-    float mx = -INFINITY;
-    for (int k = tid; k <= more; k += 256) mx = fmaxf(mx, p.part_m[part(k)]);
+    // the slot's parts, and then the slots', each by the running maximum
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = lane; k0 <= more; k0 += 4 * lanes) {
+        float pm[4], pl[4];
+        f32x4 po[4];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
-    if ((tid & 63) == 0) sm_m[tid >> 6] = mx;
+        for (int j = 0; j < 4; j++) {                     // behind the last: the last again, weighing nothing
+            const long long at = part(min(k0 + j * lanes, more));
+            pm[j] = k0 + j * lanes <= more ? p.part_m[at] : -INFINITY;
+            pl[j] = p.part_l[at];
+            po[j] = *(const f32x4*)(p.part_o + at * C + c4 * 4);
+        }
+        const float mx = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m);
+        const float a = weight(m, mx);
+        l *= a;
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] *= a;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const float w = weight(pm[j], mx);
+            if (k0 + j * lanes <= more) {
+                l = fmaf(w, pl[j], l);
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[e] = fmaf(w, po[j][e], o[e]);
+            }
+        }
+        m = mx;
+    }
+    __shared__ float sm_m[SL];
+    *(f32x4*)&sm_o[slot][c4 * 4] = o;
+    if (c4 == 0) {
+        sm_l[slot] = l;
+        sm_m[slot] = m;
+    }
     __syncthreads();
-    mx = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+    if (lane != 0 || !has_row) return;
+    float mx = m;
+    for (int k = 1; k < lanes; k++) mx = fmaxf(mx, sm_m[slot + k]);
     float lt = 0.f;
     f32x4 ot = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = pl; k <= more; k += PL) {
-        const float a = weight(p.part_m[part(k)], mx);
-        const f32x4 x = *(const f32x4*)(p.part_o + part(k) * C + c4 * 4);
-        lt = fmaf(a, p.part_l[part(k)], lt);
+    for (int k = 0; k < lanes; k++) {
+        const float w = weight(sm_m[slot + k], mx);
+        const f32x4 x = *(const f32x4*)&sm_o[slot + k][c4 * 4];
+        lt = fmaf(w, sm_l[slot + k], lt);
 #pragma unroll
-        for (int e = 0; e < 4; e++) ot[e] = fmaf(a, x[e], ot[e]);
+        for (int e = 0; e < 4; e++) ot[e] = fmaf(w, x[e], ot[e]);
     }
-    *(f32x4*)&sm_o[pl][c4 * 4] = ot;
-    if (c4 == 0) sm_l[pl] = lt;
-    __syncthreads();
-    if (tid >= LN) return;
-#pragma unroll
-    for (int k = 1; k < PL; k++) {
-        const f32x4 x = *(const f32x4*)&sm_o[k][c4 * 4];
-        lt += sm_l[k];
-#pragma unroll
-        for (int e = 0; e < 4; e++) ot[e] += x[e];
-    }
-    const float inv = lt == 0.f ? 0.f : 1.f / lt;
-    struct alignas(4 * sizeof(T)) Four { T x[4]; } v;
-#pragma unroll
-    for (int e = 0; e < 4; e++) v.x[e] = (T)(lt == 0.f ? 0.f : ot[e] * inv);
-    *(Four*)((T*)p.out + row * C + c4 * 4) = v;
-    if (c4 == 0) p.lse[row] = lt == 0.f ? -INFINITY : mx + __log2f(lt) * kLn2;
+    const int b = join.z / (p.Hkv * p.row_tiles), grp = join.z - b * p.Hkv * p.row_tiles;
+    const int h = grp / p.row_tiles, r0 = (grp - h * p.row_tiles) * kPaRows;
+    write_row<T, C>(p, (long long)b * p.H * p.N + (long long)h * (p.H / p.Hkv * p.N) + r0 + r, c4, ot, lt, mx);
 }
 
 template <typename T, int C, int BIAS, bool PF32>
 int launch_attn(const PagedAttnParams& p, hipStream_t stream) {
-    const long long blocks = p.workers ? p.workers : (long long)p.B * p.Hkv * p.row_tiles;
-    if (blocks >= (1LL << 31)) return -1;
-    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32>), dim3((unsigned)blocks), dim3(kPaThreads), 0, stream, p);
-    if (hipGetLastError() != hipSuccess) return 1;
-    if (p.workers) {
-        const int rows = p.H / p.Hkv * p.N;
-        hipLaunchKernelGGL((paged_join_kernel<T, C>), dim3((unsigned)p.workers, (unsigned)(rows < kPaRows ? rows : kPaRows)), dim3(256), 0, stream, p);
-        if (hipGetLastError() != hipSuccess) return 1;
+    if (p.workers == 0) {
+        const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;
+        if (blocks >= (1LL << 31)) return -1;
+        hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, false>), dim3((unsigned)blocks), dim3(kPaThreads), 0, stream, p);
+        return hipGetLastError() == hipSuccess ? 0 : 1;
     }
-    return 0;
+    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, true>), dim3((unsigned)((p.workers + kPaWaves - 1) / kPaWaves)), dim3(kPaThreads), 0,
+                       stream, p);
+    if (hipGetLastError() != hipSuccess) return 1;
+    const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
+    const int rows = p.H / p.Hkv * p.N < kPaRows ? p.H / p.Hkv * p.N : kPaRows;
+    // slots: as many parts at a time as a group has on average, the rest are rows
+    const long long parts = p.workers / groups;
+    const int lanes = parts >= 6 ? 8 : (parts >= 3 ? 4 : 2);
+    hipLaunchKernelGGL((paged_join_kernel<T, C>), dim3((unsigned)(p.joins_by_group ? groups : p.workers), (unsigned)((rows * lanes + 7) / 8)), dim3(2 * C),
+                       0, stream, p, lanes);
+    return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
 template <typename T, int C>
@@ -551,27 +741,35 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 
 }  // namespace
 
-// Two workgroups a CU are resident.  Requests of at most four steps are not split.
+// Waves that share the keys: all that are resident, two per SIMD.  Requests of at most 16 steps are not split.
 int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32) {
-    const int step = kPaWaves * (f32 ? 16 : 32);
+    const int step = f32 ? 16 : 32;
     const long long steps = (capacity + step - 1) / step;
-    if (steps <= 4) return 0;
+    if (steps <= 16) return 0;
     int cus = fb_cu_count();
     if (cus <= 0) cus = 256;
-    const long long most = (long long)B * Hkv * row_tiles * ((steps + kPaLeast - 1) / kPaLeast);
-    return (int)(most < 2LL * cus ? most : 2LL * cus);
+    const long long groups = (long long)B * Hkv * row_tiles;
+    if (steps * Hkv * row_tiles >= (1LL << 31)) return 0;            // a request's steps are counted in 32 bits
+    const long long most = groups * ((steps + kPaLeast - 1) / kPaLeast), all = 8LL * cus;
+    return (int)(most < all ? most : all);
 }
 
-size_t fb_paged_attn_workspace_bytes(int workers, int C) {
-    return (size_t)workers * (2 * kPaRows * (C + 2) * sizeof(float) + sizeof(int4));
+// rows: query rows of a key head
+static size_t parts_of(int workers, long long rows) { return (size_t)workers * 2 * (rows < kPaRows ? rows : kPaRows); }
+
+size_t fb_paged_attn_workspace_bytes(int workers, long long groups, long long rows, int C) {
+    return parts_of(workers, rows) * (C + 2) * sizeof(float) + (size_t)(groups < workers ? groups : workers) * sizeof(int4);
 }
 
 int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream_t stream) {
     if (p.workers) {
-        p.part_o = (float*)ws;
-        p.joins = (int4*)(p.part_o + (size_t)p.workers * 2 * kPaRows * C);
-        p.part_m = (float*)(p.joins + p.workers);
-        p.part_l = p.part_m + (size_t)p.workers * 2 * kPaRows;
+        const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
+        const size_t parts = parts_of(p.workers, (long long)(p.H / p.Hkv) * p.N);
+        p.joins_by_group = groups <= p.workers;
+        p.joins = (int4*)ws;
+        p.part_o = (float*)(p.joins + (p.joins_by_group ? groups : p.workers));
+        p.part_m = p.part_o + parts * C;
+        p.part_l = p.part_m + parts;
     }
     return f32 ? attn_channels<float>(p, C, stream) : attn_channels<bf16_t>(p, C, stream);
 }

@@ -123,11 +123,12 @@ struct PagedAttnParams {
     int B, H, Hkv, N, R, page_shift, n_pages, max_blocks, causal, phi_f32;
     float scale;
     int row_tiles;           // query rows of a key head (H / Hkv * N of them) in tiles of 16
-    int workers;             // workgroups the keys are split over; 0: one per key head and row tile, no split
-    float* part_o;           // scratch: two parts per worker, [workers, 2, 16, C]
-    float* part_m;           // [workers, 2, 16] maxima
-    float* part_l;           // [workers, 2, 16] sums
-    int4* joins;             // [workers] what the join has to do behind this worker
+    int workers;             // waves the keys are split over; 0: a workgroup per key head and row tile, no split
+    int joins_by_group;      // joins has an entry per (request, key head, row tile), else one per worker
+    float* part_o;           // scratch: two parts per worker, [workers, 2, rows, C], rows = min(16, H / Hkv * N)
+    float* part_m;           // [workers, 2, rows] maxima
+    float* part_l;           // [workers, 2, rows] sums
+    int4* joins;             // workers behind the first that have parts (0: no join), the first, the group, its rows
 };
 
 #endif
