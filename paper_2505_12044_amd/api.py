@@ -8,6 +8,7 @@ library is missing or a call returns an error status, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Callable, Optional, Tuple
 
@@ -509,52 +510,68 @@ def _need(ok: bool, what: str) -> None:
 
 def _here(*tensors: Optional[torch.Tensor]) -> None:
     """All tensors of a call live on the current device, whose stream the call goes to."""
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dev = tensors[0].get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise FlashBiasError("tensors must be CUDA tensors of the current device")
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != dev):
+        if t is not None and t.get_device() != dev:
             raise FlashBiasError("tensors must be CUDA tensors of the current device")
 
 
-def _ints(t: Optional[torch.Tensor], shape, name: str) -> None:
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
-        raise FlashBiasError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)}")
+def _ints(name: str, t: torch.Tensor, *shape: int) -> int:
+    """Address of a contiguous int32 tensor of this shape."""
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise FlashBiasError(f"{name} must be a contiguous int32 tensor of shape {shape}")
+    return t.data_ptr()
 
 
 _Six = ctypes.c_longlong * 6
-_Four = ctypes.c_int * 4
 
 
 def _row_strides(x: torch.Tensor, y: Optional[torch.Tensor]):
     """Batch, head and row strides of one or two [B,H,N,C] tensors whose channels are adjacent."""
-    for t in (x, y):
-        if t is not None and (t.dim() != 4 or t.stride(3) != 1):
-            raise FlashBiasError("tensors must be [B,H,N,C] with adjacent channels")
-    return _Six(*x.stride()[:3], *(y.stride()[:3] if y is not None else (0, 0, 0)))
+    xs = x.stride()
+    ys = (0, 0, 0, 1) if y is None else y.stride()
+    if len(xs) != 4 or len(ys) != 4 or xs[3] != 1 or ys[3] != 1:
+        raise FlashBiasError("tensors must be [B,H,N,C] with adjacent channels")
+    return _Six(xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
+
+
+@functools.lru_cache(maxsize=64)
+def _sections(sections: Tuple[int, ...]):
+    """(axes, pairs, the C array) of the pairs of each axis."""
+    _need(1 <= len(sections) <= 4, "one to four axes")
+    return len(sections), sum(sections), (ctypes.c_int * 4)(*sections)
 
 
 def _rotary(lib_fn, what, x0, x1, positions, freqs, sections, interleaved, out, stream):
     strides = _row_strides(x0, x1)
-    _here(x0, x1, positions, freqs, *(out or ()))
+    _here(x0, x1, positions, freqs)
     B, H0, N, C = x0.shape
-    sections = tuple(int(s) for s in sections)
-    _need(1 <= len(sections) <= 4, "one to four axes")
-    _need(x1 is None or (x1.dtype == x0.dtype and x1.shape[0] == B and tuple(x1.shape[2:]) == (N, C)),
-          "both tensors must have one dtype, batch, length and head dimension")
-    _need(positions.dtype in (torch.int32, torch.float32) and positions.is_contiguous() and positions.dim() == 3 and
-          positions.shape[0] == len(sections) and positions.shape[1] in (1, B) and positions.shape[2] == N,
+    dtype = x0.dtype
+    axes, pairs, c_sections = _sections(tuple(sections))
+    H1 = 0
+    if x1 is not None:
+        H1 = x1.shape[1]
+        _need(x1.dtype is dtype and x1.shape == (B, H1, N, C), "both tensors must have one dtype, batch, length and head dimension")
+    f32_pos = positions.dtype is torch.float32
+    shape = positions.shape
+    _need((f32_pos or positions.dtype is torch.int32) and (shape == (axes, B, N) or shape == (axes, 1, N)) and positions.is_contiguous(),
           "positions must be a contiguous int32 or float32 tensor [axes, B or 1, N]")
-    _need(freqs.dtype == torch.float32 and freqs.is_contiguous() and freqs.numel() == sum(sections),
+    _need(freqs.dtype is torch.float32 and freqs.numel() == pairs and freqs.is_contiguous(),
           "freqs must be a contiguous float32 tensor with one entry per pair")
     if out is None:
-        out = (torch.empty((B, H0, N, C), dtype=x0.dtype, device=x0.device),
-               None if x1 is None else torch.empty((B, x1.shape[1], N, C), dtype=x0.dtype, device=x0.device))
-    y0, y1 = out
-    for x, y in ((x0, y0), (x1, y1)):
-        _need((x is None) == (y is None) and (x is None or (y.shape == x.shape and y.dtype == x.dtype)),
-              "outputs must have their inputs' shapes and dtype")
-    st = lib_fn(x0.data_ptr(), _ptr(y0), H0, None if x1 is None else x1.data_ptr(), _ptr(y1), 0 if x1 is None else x1.shape[1],
-                strides, positions.data_ptr(), int(positions.dtype == torch.float32), int(positions.shape[1] == 1),
-                freqs.data_ptr(), _Four(*sections), B, N, C, int(bool(interleaved)), _dtype_code(x0), _stream(stream))
+        y0 = x0.new_empty((B, H0, N, C))
+        y1 = None if x1 is None else x0.new_empty((B, H1, N, C))
+    else:
+        y0, y1 = out
+        for x, y in ((x0, y0), (x1, y1)):
+            _need((x is None) == (y is None) and (x is None or (y.shape == x.shape and y.dtype is dtype and y.is_contiguous())),
+                  "outputs must be contiguous, with their inputs' shapes and dtype")
+        _here(y0, y1)
+    st = lib_fn(x0.data_ptr(), y0.data_ptr(), H0, None if x1 is None else x1.data_ptr(), None if y1 is None else y1.data_ptr(), H1,
+                strides, positions.data_ptr(), f32_pos, shape[1] == 1, freqs.data_ptr(), c_sections, B, N, C, bool(interleaved),
+                _dtype_code(x0), _stream(stream))
     _check(st, what)
     return y0, y1
 
@@ -579,37 +596,38 @@ def fb_paged_plan(lens, new_lens, table, ring, state, n_new: int, page: int, len
     free pages, int32, in place), and the up to n_new new tokens of each are mapped.  Returns lens [B] and state [2]
     (ring head, free pages) afterwards, slots [B, n_new] (-1: no token) and positions [B, n_new]."""
     lib = load_library()
-    B = lens.shape[0]
     _here(lens, new_lens, table, ring, state, lens_out, state_out, slots, positions)
-    _ints(lens, (B,), "lens")
-    _ints(new_lens, (B,), "new_lens")
-    _need(table.dim() == 2, "table must be [B, max_blocks]")
-    _ints(table, (B, table.shape[1]), "table")
-    _ints(ring, (ring.numel(),), "ring")
-    _ints(state, (2,), "state")
+    _need(lens.dim() == 1 and table.dim() == 2 and ring.dim() == 1, "lens, ring: one dimension, table: [B, max_blocks]")
+    B, blocks, n_pages = lens.shape[0], table.shape[1], ring.shape[0]
     new = lens.new_empty
-    lens_out = new((B,)) if lens_out is None else lens_out
-    state_out = new((2,)) if state_out is None else state_out
-    slots = new((B, n_new)) if slots is None else slots
-    positions = new((B, n_new)) if positions is None else positions
-    _ints(lens_out, (B,), "lens_out")
-    _ints(state_out, (2,), "state_out")
-    _ints(slots, (B, n_new), "slots")
-    _ints(positions, (B, n_new), "positions")
-    st = lib.fb_paged_plan(lens.data_ptr(), new_lens.data_ptr(), table.data_ptr(), ring.data_ptr(), state.data_ptr(),
-                           lens_out.data_ptr(), state_out.data_ptr(), slots.data_ptr(), positions.data_ptr(),
-                           B, n_new, page, ring.numel(), table.shape[1], _stream(stream))
+    if lens_out is None:
+        lens_out = new(B)
+    if state_out is None:
+        state_out = new(2)
+    if slots is None:
+        slots = new((B, n_new))
+    if positions is None:
+        positions = new((B, n_new))
+    st = lib.fb_paged_plan(_ints("lens", lens, B), _ints("new_lens", new_lens, B), _ints("table", table, B, blocks),
+                           _ints("ring", ring, n_pages), _ints("state", state, 2), _ints("lens_out", lens_out, B),
+                           _ints("state_out", state_out, 2), _ints("slots", slots, B, n_new), _ints("positions", positions, B, n_new),
+                           B, n_new, page, n_pages, blocks, _stream(stream))
     _check(st, "fb_paged_plan")
     return lens_out, state_out, slots, positions
 
 
-def _check_pages(k_pages, v_pages, phi_pages, R, phi_dtype):
-    _need(k_pages.dim() == 4 and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype,
+def _check_pages(k_pages, v_pages, phi_pages, factors):
+    """(n_pages, Hkv, page, C, R) of a cache and the factors that meet it."""
+    shape = k_pages.shape
+    _need(len(shape) == 4 and v_pages.shape == shape and v_pages.dtype is k_pages.dtype,
           "k_pages and v_pages must be [n_pages, Hkv, page, C] of one dtype")
-    _need((phi_pages is None) == (R == 0), "factors need their pages")
-    if R:
-        _need(tuple(phi_pages.shape) == (*k_pages.shape[:3], R) and phi_pages.dtype == phi_dtype,
-              "phi_pages must be [n_pages, Hkv, page, R] of the factors' dtype")
+    if factors is None:
+        _need(phi_pages is None, "factors need their pages")
+        return (*shape, 0)
+    R = factors.shape[-1]
+    _need(phi_pages is not None and phi_pages.shape == (*shape[:3], R) and phi_pages.dtype is factors.dtype,
+          "phi_pages must be [n_pages, Hkv, page, R] of the factors' dtype")
+    return (*shape, R)
 
 
 def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, phi_batch_broadcast: Optional[bool] = None,
@@ -620,20 +638,25 @@ def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, p
     strides = _row_strides(k, v)
     _here(k, v, slots, k_pages, v_pages, phi_k, phi_pages)
     B, Hkv, N, C = k.shape
-    R = 0 if phi_k is None else phi_k.shape[-1]
-    _check_pages(k_pages, v_pages, phi_pages, R, None if phi_k is None else phi_k.dtype)
-    n_pages, hp, page, cp = k_pages.shape
-    _need(v.shape == k.shape and k.dtype == v.dtype == k_pages.dtype and (hp, cp) == (Hkv, C),
+    n_pages, hp, page, cp, R = _check_pages(k_pages, v_pages, phi_pages, phi_k)
+    _need(v.shape == k.shape and k.dtype is v.dtype and k.dtype is k_pages.dtype and hp == Hkv and cp == C,
           "k, v and their pages must have one dtype, head count and head dimension")
-    _need(R == 0 or (phi_k.shape[0] in (1, B) and tuple(phi_k.shape[1:]) == (Hkv, N, R)), "phi_k must be [B or 1,Hkv,N,R]")
-    _ints(slots, (B, N), "slots")
-    if phi_batch_broadcast is None:
-        phi_batch_broadcast = R > 0 and phi_k.shape[0] == 1 and B > 1
-    code = _dtype_code(k)
-    st = lib.fb_paged_append(k.data_ptr(), v.data_ptr(), _ptr(phi_k), slots.data_ptr(), _ptr(k_pages), _ptr(v_pages),
-                             _ptr(phi_pages), strides, B, Hkv, N, C, R, page, n_pages, code,
-                             _dtype_code(phi_k) if R else code, int(bool(phi_batch_broadcast)), _stream(stream))
+    code = phi_code = _dtype_code(k)
+    if R:
+        _need(phi_k.shape == (B, Hkv, N, R) or phi_k.shape == (1, Hkv, N, R), "phi_k must be [B or 1,Hkv,N,R]")
+        phi_code = _dtype_code(phi_k)
+        if phi_batch_broadcast is None:
+            phi_batch_broadcast = phi_k.shape[0] == 1 and B > 1
+    st = lib.fb_paged_append(k.data_ptr(), v.data_ptr(), _ptr(phi_k), _ints("slots", slots, B, N), _ptr(k_pages), _ptr(v_pages),
+                             _ptr(phi_pages), strides, B, Hkv, N, C, R, page, n_pages, code, phi_code,
+                             bool(phi_batch_broadcast), _stream(stream))
     _check(st, "fb_paged_append")
+
+
+@functools.lru_cache(maxsize=256)
+def _paged_attn_workspace(device, B, H, Hkv, N, C, page, max_blocks, dtype_code) -> int:
+    """The size query, once for each shape (it depends on the device's CU count too)."""
+    return int(load_library().fb_paged_attn_fwd_workspace_bytes(B, H, Hkv, N, C, page, max_blocks, dtype_code))
 
 
 def fb_paged_attn_fwd_workspace_bytes(B, H, Hkv, N, C, page, max_blocks, dtype_code=FB_BF16) -> int:
@@ -651,36 +674,37 @@ def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None,
     workspace allocates nothing and does without (a key head is then not split over the GPU)."""
     lib = load_library()
     _here(q, k_pages, v_pages, table, lens, starts, phi_q, phi_pages, slopes, out, lse, workspace)
+    _need(q.dim() == 4 and table.dim() == 2, "q must be [B,H,N,C], table [B, max_blocks]")
     B, H, N, C = q.shape
-    R = 0 if phi_q is None else phi_q.shape[-1]
-    _check_pages(k_pages, v_pages, phi_pages, R, None if phi_q is None else phi_q.dtype)
-    n_pages, Hkv, page, cp = k_pages.shape
-    _need(k_pages.dtype == q.dtype and cp == C, "q and the pages must have one dtype and head dimension")
-    _need(R == 0 or (phi_q.shape[0] in (1, B) and tuple(phi_q.shape[1:]) == (H, N, R)), "phi_q must be [B or 1,H,N,R]")
-    _need(slopes is None or (slopes.dtype == torch.float32 and slopes.numel() == H),
-          "slopes must be a float32 tensor with one entry per head")
-    _need(table.dim() == 2, "table must be [B, max_blocks]")
     blocks = table.shape[1]
-    _ints(table, (B, blocks), "table")
-    _ints(lens, (B,), "lens")
-    _ints(starts, (B,), "starts")
-    if phi_batch_broadcast is None:
-        phi_batch_broadcast = R > 0 and phi_q.shape[0] == 1 and B > 1
-    code = _dtype_code(q)
-    if workspace is None and (out is None or lse is None):
-        need = int(lib.fb_paged_attn_fwd_workspace_bytes(B, H, Hkv, N, C, page, blocks, code))
-        workspace = _scratch(need, q.device, stream) if need else None
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    n_pages, Hkv, page, cp, R = _check_pages(k_pages, v_pages, phi_pages, phi_q)
+    _need(k_pages.dtype is q.dtype and cp == C, "q and the pages must have one dtype and head dimension")
+    code = phi_code = _dtype_code(q)
+    if R:
+        _need(phi_q.shape == (B, H, N, R) or phi_q.shape == (1, H, N, R), "phi_q must be [B or 1,H,N,R]")
+        phi_code = _dtype_code(phi_q)
+        if phi_batch_broadcast is None:
+            phi_batch_broadcast = phi_q.shape[0] == 1 and B > 1
+    if slopes is not None:
+        _need(slopes.dtype is torch.float32 and slopes.numel() == H, "slopes must be a float32 tensor with one entry per head")
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.numel() * workspace.element_size()
+    elif out is None or lse is None:
+        ws_bytes = _paged_attn_workspace(q.get_device(), B, H, Hkv, N, C, page, blocks, code)
+        if ws_bytes:
+            workspace = _scratch(ws_bytes, q.device, stream)
     if out is None:
         out = torch.empty_like(q)
+    else:
+        _need(out.shape == q.shape and out.dtype is q.dtype, "out must be like q")
     if lse is None:
-        lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
-    _need(out.shape == q.shape and out.dtype == q.dtype and tuple(lse.shape) == (B, H, N) and lse.dtype == torch.float32,
-          "out must be like q, lse [B,H,N] float32")
+        lse = q.new_empty((B, H, N), dtype=torch.float32)
+    else:
+        _need(lse.shape == (B, H, N) and lse.dtype is torch.float32, "lse must be [B,H,N] float32")
     st = lib.fb_paged_attn_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(phi_q), _ptr(phi_pages), _ptr(slopes),
-                               table.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr(),
-                               _ptr(out), _ptr(lse), B, H, Hkv, N, C, R, page, n_pages, blocks, int(bool(causal)),
-                               code, _dtype_code(phi_q) if R else code, int(bool(phi_batch_broadcast)), float(scale),
-                               _ptr(workspace), ws_bytes, _stream(stream))
+                               _ints("table", table, B, blocks), _ints("lens", lens, B), None if starts is None else _ints("starts", starts, B),
+                               _ptr(out), _ptr(lse), B, H, Hkv, N, C, R, page, n_pages, blocks, bool(causal), code, phi_code,
+                               bool(phi_batch_broadcast), scale, _ptr(workspace), ws_bytes, _stream(stream))
     _check(st, "fb_paged_attn_fwd")
     return out, lse

@@ -756,6 +756,7 @@ int fb_paged_attn_fwd(const void* q, const void* k_pages, const void* v_pages,
     if (!q || !k_pages || !v_pages || !table || !lens || !out || !lse) return FB_ERR_NULL;
     if (int st = check_common(B, H, N, C, R)) return st;
     if (Hkv <= 0 || H % Hkv != 0 || max_blocks <= 0) return FB_ERR_SHAPE;
+    if ((long long)(H / Hkv) * N >= (1 << 24)) return FB_ERR_SHAPE;
     if ((long long)B * max_blocks >= (1LL << 31)) return FB_ERR_SHAPE;
     if (R > 0 && (!phi_q || !phi_pages)) return FB_ERR_NULL;
     if (int st = check_pages(page, n_pages)) return st;

@@ -31,7 +31,23 @@ namespace {
 constexpr int kPaWaves = 4;
 constexpr int kPaThreads = kPaWaves * 64;
 constexpr int kPaRows = 16;
-constexpr int kPaLeast = 4;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
+#ifndef PA_DIRECT
+#define PA_DIRECT 512
+#endif
+#ifndef PA_LEAST
+#define PA_LEAST 2
+#endif
+#ifndef PA_GB
+#define PA_GB(C) 2
+#endif
+#ifndef PA_GF
+#define PA_GF(C) 1
+#endif
+constexpr int kPaLeast = PA_LEAST;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
+#ifndef PA_LEAD
+#define PA_LEAD 2
+#endif
+constexpr int kPaLead = PA_LEAD;        // steps that a group's beginning and end cost, counted into the shares
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
@@ -57,13 +73,15 @@ FB_DEV float column_sum(float x) {
 FB_DEV float weight(float a, float m) { return a == -INFINITY ? 0.f : fast_exp2((a - m) * kLog2e); }
 
 // ---- one step of a wave: KW keys against 16 rows -----------------------------------------------
+// KW: as many as 64 registers of keys and values hold, up to 64 (a wave has one step in flight, and a step takes a
+// memory latency at least: 32 keys a step at 64 channels are slower).
 // Lane l: g = l / 16, i = l % 16.  S^T group s (16 keys): column i (the query row), keys 4 g + r.
 template <typename T, int C>
 struct Step;
 
 template <int C>
 struct Step<bf16_t, C> {
-    static constexpr int KW = 32, GROUPS = 2, NV = C / 16;
+    static constexpr int GROUPS = PA_GB(C), KW = 16 * GROUPS, NV = C / 16;
     static constexpr int NU = C >= 32 ? C / 32 : 1;
     using KVec = std::conditional_t<C == 16, u32x2, u32x4>;
     using VVec = std::conditional_t<NV == 8, u32x4, std::conditional_t<NV == 4, u32x2, std::conditional_t<NV == 2, unsigned, unsigned short>>>;
@@ -93,14 +111,15 @@ struct Step<bf16_t, C> {
         }
         return acc;
     }
-    struct Probs { bf16x8 hi, lo; };
+    struct Probs { bf16x8 hi[GROUPS / 2], lo[GROUPS / 2]; };       // two key groups an operand
     static FB_DEV Probs probs(const f32x4 (&p)[GROUPS]) {
         Probs w;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
+        for (int e = 0; e < 4 * GROUPS; e++) {
             const float x = p[e / 4][e % 4];
-            w.hi[e] = (bf16_t)x;
-            w.lo[e] = (bf16_t)(x - (float)w.hi[e]);
+            const bf16_t hi = (bf16_t)x;
+            w.hi[e / 8][e % 8] = hi;
+            w.lo[e / 8][e % 8] = (bf16_t)(x - (float)hi);
         }
         return w;
     }
@@ -110,20 +129,24 @@ struct Step<bf16_t, C> {
         if constexpr (NV <= 2) return x;
         else return x[w];
     }
-    // o[t] += channel t's values times the probabilities
+    // o + channel t's values times the probabilities
     static FB_DEV f32x4 product(const Values& v, int t, const Probs& p, f32x4 o) {
-        u32x4 a;
 #pragma unroll
-        for (int j = 0; j < 4; j++)
-            a[j] = __builtin_amdgcn_perm(word(v, 2 * j + 1, t / 2), word(v, 2 * j, t / 2), t % 2 ? 0x07060302u : 0x05040100u);
-        o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), p.hi, o, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), p.lo, o, 0, 0, 0);
+        for (int s = 0; s < GROUPS / 2; s++) {
+            u32x4 a;
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                a[j] = __builtin_amdgcn_perm(word(v, 8 * s + 2 * j + 1, t / 2), word(v, 8 * s + 2 * j, t / 2), t % 2 ? 0x07060302u : 0x05040100u);
+            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), p.hi[s], o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), p.lo[s], o, 0, 0, 0);
+        }
+        return o;
     }
 };
 
 template <int C>
 struct Step<float, C> {
-    static constexpr int KW = 16, GROUPS = 1, NV = C / 16;
+    static constexpr int GROUPS = PA_GF(C), KW = 16 * GROUPS, NV = C / 16;
     static constexpr int NU = C / 16;
     using VVec = std::conditional_t<NV == 8, f32x8, std::conditional_t<NV == 4, f32x4, std::conditional_t<NV == 2, f32x2, float>>>;
     struct Query { f32x4 x[NU]; };
@@ -147,85 +170,95 @@ struct Step<float, C> {
             for (int e = 0; e < 4; e++) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[s][u][e], q.x[u][e], acc, 0, 0, 0);
         return acc;
     }
-    struct Probs { f32x4 x; };
-    static FB_DEV Probs probs(const f32x4 (&p)[GROUPS]) { return Probs{p[0]}; }
+    struct Probs { f32x4 x[GROUPS]; };
+    static FB_DEV Probs probs(const f32x4 (&p)[GROUPS]) {
+        Probs w;
+#pragma unroll
+        for (int s = 0; s < GROUPS; s++) w.x[s] = p[s];
+        return w;
+    }
     static FB_DEV f32x4 product(const Values& v, int t, const Probs& p, f32x4 o) {
 #pragma unroll
-        for (int r = 0; r < 4; r++) {
-            float a;
-            if constexpr (NV == 1) a = v.x[0][r];
-            else a = v.x[0][r][t];
-            o = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p.x[r], o, 0, 0, 0);
-        }
+        for (int s = 0; s < GROUPS; s++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                float a;
+                if constexpr (NV == 1) a = v.x[s][r];
+                else a = v.x[s][r][t];
+                o = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p.x[s][r], o, 0, 0, 0);
+            }
         return o;
     }
 };
 
-enum { kBiasNone = 0, kBiasAlibi = 1, kBiasFactors4 = 2, kBiasFactors = 3 };    // factors: up to 4, any number
+// factors: up to four; up to 16, a multiple of four; any number
+enum { kBiasNone = 0, kBiasAlibi = 1, kBiasFactors4 = 2, kBiasFactors16 = 3, kBiasFactors = 4 };
 
 // Arrays that are not written while the kernel runs, read at wave-uniform places: scalar loads, which do not queue behind
 // the rows in flight.
 typedef const __attribute__((address_space(4))) int* ConstInts;
 FB_DEV ConstInts const_ints(const int* x) { return (ConstInts)(uintptr_t)x; }
 
-FB_DEV int held_keys(const PagedAttnParams& p, int b) {
-    return max((int)min((long long)const_ints(p.lens)[b], (long long)p.max_blocks << p.page_shift), 0);
-}
+// Keys of a request: its length within the table (capacity: 31 bits).
+FB_DEV int held_keys(const PagedAttnParams& p, int len) { return max(min(len, p.capacity), 0); }
 
 // Steps of a request per group; one that holds nothing has one too (its rows are written).
 template <int KW>
-FB_DEV int steps_of(int len) { return len > KW ? (len + KW - 1) / KW : 1; }
+FB_DEV int steps_of(int len) { return len > KW ? (int)((unsigned)(len + KW - 1) / KW) : 1; }
 
-// Inclusive sums over the wave.
-FB_DEV long long wave_scan(long long x) {
+// Sums up to the lane's.
+FB_DEV int wave_scan(int x) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const long long y = __shfl_up(x, d);
+        const int y = __shfl_up(x, d);
         if (lane >= d) x += y;
     }
     return x;
 }
 
-// The steps of all requests laid end to end, cut in equal shares: where this wave's begins and ends.  `total`, `workers`
-// (those that have a share), `u`, `u_end`: steps; b, rem: the request that step u lies in and its place there.
+// The costs of all requests' groups (their steps, and kPaLead that lie before them) laid end to end and cut in shares of
+// `base` or, the first `longer` of them, base + 1: this wave's is [u, u_end), u lies in request b, rem behind its beginning.
+// All below 2^31 (the launch sees to it).
 struct Share {
-    long long total, u, u_end, rem;
-    int workers, b;
+    int u, u_end, b, rem;
+    int base, longer, workers;
+    FB_DEV void cut(int total, int most, int worker) {
+        workers = min(most, (total + kPaLeast - 1) / kPaLeast);
+        base = total / workers;
+        longer = total - base * workers;
+        u = worker * base + min(worker, longer);
+        u_end = worker < workers ? u + base + (worker < longer ? 1 : 0) : u;
+    }
+    FB_DEV int worker_of(int x) const {
+        const int edge = longer * (base + 1);
+        return x < edge ? x / (base + 1) : longer + (x - edge) / base;
+    }
 };
 
 template <int KW>
 FB_DEV Share share_of(const PagedAttnParams& p, int groups, int worker) {
-    __shared__ long long sm_sum[kPaWaves];
-    __shared__ long long sm_rem[kPaWaves];
-    __shared__ int sm_b[kPaWaves];
+    __shared__ int sm_sum[kPaWaves], sm_b[kPaWaves], sm_rem[kPaWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Share s{};
-    const auto cut = [&]() {
-        s.workers = (int)min((long long)p.workers, (s.total + kPaLeast - 1) / kPaLeast);
-        s.u = worker * s.total / s.workers;
-        s.u_end = worker < s.workers ? (worker + 1) * s.total / s.workers : s.u;
-    };
+    const auto cost = [&](int b) { return b < p.B ? (steps_of<KW>(held_keys(p, p.lens[b])) + kPaLead) * groups : 0; };
     if (p.B <= 64) {                                     // every wave by itself
-        const long long own = lane < p.B ? (long long)steps_of<KW>(max((int)min((long long)p.lens[lane], (long long)p.max_blocks << p.page_shift), 0)) * groups : 0;
-        const long long end = wave_scan(own);
-        s.total = __shfl(end, 63);
-        cut();
+        const int own = cost(lane), end = wave_scan(own);
+        s.cut(__builtin_amdgcn_readlane(end, 63), p.workers, worker);
         if (s.u < s.u_end) {
             s.b = __builtin_ctzll(__ballot(end > s.u));
-            s.rem = s.u - __shfl(end - own, s.b);
+            s.rem = s.u - __builtin_amdgcn_readlane(end - own, s.b);
         }
         return s;
     }
     // the workgroup's four shares together, 256 requests at a time: the total first
-    const auto tile = [&](int b0, long long& own, long long& sum) {
-        const int b = b0 + tid;
-        own = b < p.B ? (long long)steps_of<KW>(max((int)min((long long)p.lens[b], (long long)p.max_blocks << p.page_shift), 0)) * groups : 0;
-        const long long in_wave = wave_scan(own);
+    const auto tile = [&](int b0, int& own, int& sum) {
+        own = cost(b0 + tid);
+        const int in_wave = wave_scan(own);
         __syncthreads();
         if (lane == 63) sm_sum[wave] = in_wave;
         __syncthreads();
-        long long before = 0;
+        int before = 0;
         sum = 0;
 #pragma unroll
         for (int w = 0; w < kPaWaves; w++) {
@@ -234,18 +267,16 @@ FB_DEV Share share_of(const PagedAttnParams& p, int groups, int worker) {
         }
         return before + in_wave;
     };
-    long long own, sum;
+    int own, sum, total = 0, before = 0;
     for (int b0 = 0; b0 < p.B; b0 += kPaThreads) {
         tile(b0, own, sum);
-        s.total += sum;
+        total += sum;
     }
-    cut();
-    long long before = 0;
+    s.cut(total, p.workers, worker);
     for (int b0 = 0; b0 < p.B; b0 += kPaThreads) {
-        const long long end = before + tile(b0, own, sum);
+        const int end = before + tile(b0, own, sum);
         for (int w = 0; w < kPaWaves; w++) {
-            const int k = worker - wave + w;
-            const long long u = k * s.total / s.workers;
+            const int k = worker - wave + w, u = k * s.base + min(k, s.longer);
             if (end - own <= u && u < end) {
                 sm_b[w] = b0 + tid;
                 sm_rem[w] = u - (end - own);
@@ -272,7 +303,7 @@ FB_DEV void write_row(const PagedAttnParams& p, long long row, int c4, const f32
 
 // One wave's (SPLIT) or workgroup's part of a group: steps t0..t1 of n_steps.
 struct Segment {
-    int b, len, n_steps, grp, t0, t1;
+    int b, len, start, n_steps, grp, t0, t1;
 };
 
 // BIAS, PF32: kind of bias and whether the factors are float
@@ -281,217 +312,201 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
     using S = Step<T, C>;
     constexpr int KW = S::KW, NV = S::NV, GROUPS = S::GROUPS;
     constexpr int STRIDE = SPLIT ? KW : kPaWaves * KW;    // keys from one step of a wave to its next
-    constexpr int NF = BIAS == kBiasFactors4 ? 1 : (BIAS == kBiasFactors ? 4 : 0);
+    constexpr int NF = BIAS == kBiasFactors4 ? 1 : (BIAS >= kBiasFactors16 ? 4 : 0);
     using PT = std::conditional_t<PF32, float, bf16_t>;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, i = lane & 15;
     const int groups = p.Hkv * p.row_tiles;               // of a request
-    const int rows_all = p.H / p.Hkv * p.N;
-    const int part_rows = min(kPaRows, rows_all);
+    const int rows_all = p.G * p.N;
     const int page_mask = (1 << p.page_shift) - 1;
 
-    Segment seg;
+    auto enter = [&](Segment& s) __attribute__((always_inline)) {          // request s.b
+        s.len = held_keys(p, const_ints(p.lens)[s.b]);
+        s.n_steps = steps_of<KW>(s.len);
+        s.start = p.starts ? min(max(const_ints(p.starts)[s.b], -(1 << 30)), 1 << 30) : s.len - p.N;
+    };
+    Segment f;                                            // of the step to load next, at key fk
     Share share{};
     const int worker = blockIdx.x * kPaWaves + wave;
-    long long left = 0;                                   // steps of this worker behind the segment
+    int left = 0;                                         // of this worker's share behind that segment
     if constexpr (SPLIT) {
         share = share_of<KW>(p, groups, worker);
-        if (share.u >= share.u_end) {
+        f.b = __builtin_amdgcn_readfirstlane(share.b);
+        left = __builtin_amdgcn_readfirstlane(share.u_end - share.u);
+        f.t0 = f.t1 = 0;
+        if (left > 0) {
+            enter(f);
+            const int rem = __builtin_amdgcn_readfirstlane(share.rem), cost = f.n_steps + kPaLead;
+            f.grp = __builtin_amdgcn_readfirstlane((int)((unsigned)rem / (unsigned)cost));
+            const int at = rem - f.grp * cost;            // the share's beginning in the group's costs
+            f.t0 = max(at - kPaLead, 0);
+            f.t1 = max(min(f.n_steps, at - kPaLead + left), 0);
+            left -= f.t1 + kPaLead - at;
+        }
+        if (f.t1 <= f.t0) {                               // no share, or all of it before a group's first step
             if (!p.joins_by_group && worker < p.workers && lane == 0) p.joins[worker] = make_int4(0, 0, 0, 0);
             return;
         }
-        seg.b = __builtin_amdgcn_readfirstlane(share.b);
-        seg.len = held_keys(p, seg.b);
-        seg.n_steps = steps_of<KW>(seg.len);
-        const unsigned rem = __builtin_amdgcn_readfirstlane((int)share.rem);      // < groups * steps of one request < 2^31
-        seg.grp = (int)(rem / (unsigned)seg.n_steps);
-        seg.t0 = (int)rem - seg.grp * seg.n_steps;
-        left = share.u_end - share.u;
-        left = ((long long)__builtin_amdgcn_readfirstlane((int)(left >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)left);
-        seg.t1 = (int)min((long long)seg.n_steps, seg.t0 + left);
-        left -= seg.t1 - seg.t0;
     } else {
-        seg.b = blockIdx.x / groups;
-        seg.grp = blockIdx.x - seg.b * groups;
-        seg.len = held_keys(p, seg.b);
-        seg.t0 = 0;
-        seg.t1 = seg.n_steps = steps_of<KW>(seg.len);
+        f.b = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)groups);
+        f.grp = blockIdx.x - f.b * groups;
+        enter(f);
+        f.t0 = 0;
+        f.t1 = f.n_steps;
     }
-    int4 join = make_int4(0, 0, 0, 0);
 
     // ---- what a step reads ----
-    // pages of the 16-key groups from key k on (-1 behind `end`), and the first row of each in its page; a group whose page is
-    // none is not visible, and the first rows of page 0 stand in for it
-    auto pages_at = [&](int (&page)[GROUPS], const Segment& s, int k, int end) __attribute__((always_inline)) {
+    // Pages of the 16-key groups, -1 behind the segment and for an entry that is no page: such a group is not visible, and the
+    // first rows of page 0 stand in for it.
+    auto pages_at = [&](int (&page)[GROUPS], const Segment& s, int k) __attribute__((always_inline)) {
         const ConstInts table = const_ints(p.table) + (long long)s.b * p.max_blocks;
+        const int end = min(s.len, s.t1 * KW);
 #pragma unroll
-        for (int x = 0; x < GROUPS; x++) page[x] = k + 16 * x < end ? table[(k + 16 * x) >> p.page_shift] : -1;
+        for (int x = 0; x < GROUPS; x++) {
+            const int held = table[max(min(k + 16 * x, end - 1), 0) >> p.page_shift];
+            page[x] = k + 16 * x < end && (unsigned)held < (unsigned)p.n_pages ? held : -1;
+        }
     };
-    auto rows_of = [&](long long (&row)[GROUPS], const int (&page)[GROUPS], int h, int k) __attribute__((always_inline)) {
-#pragma unroll
-        for (int x = 0; x < GROUPS; x++)
-            row[x] = (unsigned)page[x] < (unsigned)p.n_pages
-                         ? (((long long)page[x] * p.Hkv + h) << p.page_shift) + ((k + 16 * x) & page_mask) : -1;
+    auto row_at = [&](int page, int h, int k) __attribute__((always_inline)) {      // row of key k, the first of a group
+        return page < 0 ? 0LL : (((long long)page * p.Hkv + h) << p.page_shift) + (k & page_mask);
     };
     typename S::Keys kr;
     typename S::Values vr;
-    PT fr[GROUPS][NF > 0 ? NF : 1];
-    // Factors of one row, the lane's share: factor g (up to four), or 4 g .. 4 g + 3 of the first 16, at once where rows allow.
-    const bool factors_x4 = NF == 4 && p.R % 4 == 0;
-    auto load_factors = [&](PT (&f)[NF > 0 ? NF : 1], const PT* pk) __attribute__((always_inline)) {
-        if (factors_x4) {
-            struct alignas(4 * sizeof(PT)) Four { PT x[4]; } v = {};
+    unsigned fr[GROUPS][NF > 0 ? NF : 1];                 // factors as loaded (unpacking them would wait for the load)
+    // Factors of one row, the lane's share: factor g of up to four; 4 g .. 4 g + 3 of the first 16.
+    auto load_factors = [&](unsigned (&f)[NF > 0 ? NF : 1], const PT* pk) __attribute__((always_inline)) {
+        using Bits = std::conditional_t<PF32, unsigned, unsigned short>;
+        if constexpr (BIAS == kBiasFactors16) {
+            using Four = std::conditional_t<PF32, u32x4, u32x2>;
+            Four v = {};
             if (4 * g < p.R) v = *(const Four*)(pk + 4 * g);
 #pragma unroll
-            for (int y = 0; y < NF; y++) f[y] = v.x[y];
+            for (int y = 0; y < (PF32 ? 4 : 2); y++) f[y] = v[y];
         } else {
 #pragma unroll
-            for (int y = 0; y < NF; y++) f[y] = NF * g + y < p.R ? pk[NF * g + y] : (PT)0.f;
-        }
-    };
-    auto load_keys = [&](const long long (&row)[GROUPS]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int x = 0; x < GROUPS; x++) {
-            const long long at = row[x] >= 0 ? row[x] : 0;
-            S::load_keys(kr, x, (const T*)p.k_pages + at * C, g, i);
-            if constexpr (NF > 0) {
-                load_factors(fr[x], (const PT*)p.phi_pages + (at + i) * p.R);
+            for (int y = 0; y < NF; y++) {
+                f[y] = 0u;
+                if (NF * g + y < p.R) f[y] = ((const Bits*)pk)[NF * g + y];
             }
         }
     };
-    auto load_values = [&](const long long (&row)[GROUPS]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int x = 0; x < GROUPS; x++) S::load_values(vr, x, (const T*)p.v_pages + (row[x] >= 0 ? row[x] : 0) * C, g, i);
+    auto factor = [&](const unsigned (&f)[NF > 0 ? NF : 1], int y) __attribute__((always_inline)) {
+        if constexpr (PF32) return __builtin_bit_cast(float, f[y]);
+        else if constexpr (BIAS == kBiasFactors16) return __builtin_bit_cast(float, y & 1 ? f[y / 2] & 0xffff0000u : f[y / 2] << 16);
+        else return __builtin_bit_cast(float, f[y] << 16);
     };
-    auto first_key = [&](const Segment& s) { return s.t0 * KW + (SPLIT ? 0 : wave * KW); };
-    auto key_end = [&](const Segment& s) { return min(s.len, s.t1 * KW); };
 
-    // One step ahead: the next keys are loaded when the scores have used this step's, the next values after this step's
-    // product; the next segment's first step counts as the last step's next.  Pages are read a step before that.
-    long long row[GROUPS], next[GROUPS];
-    int page[GROUPS];
-    pages_at(page, seg, first_key(seg), key_end(seg));
-    rows_of(row, page, seg.grp / p.row_tiles, first_key(seg));
-    if (first_key(seg) < key_end(seg)) {
-        load_keys(row);
-        load_values(row);
-    }
+    // One loop over the steps of all segments, one step ahead: the next step's keys are loaded when the scores have used this
+    // one's, its values after this one's product, its pages before that.  (The first turn only loads: the code is walked
+    // through cold by every CU, and a second copy of the loads costs more than it saves.)
+    Segment s = f;
+    int fk = f.t0 * KW + (SPLIT ? 0 : wave * KW), k0 = 0;
+    int f_page[GROUPS], page[GROUPS];
+    pages_at(f_page, f, fk);
+    bool have = false, more = true;                       // a step is loaded; one is to be loaded
+
+    // of the segment: the lane's query row, its sums
+    bool has_row = false;
+    int pos = 0, limit = 0, all_see = 0, rows = 0, h = 0;
+    long long row_base = 0;
+    typename S::Query q = {};
+    float phi_q[NF > 0 ? NF : 1] = {}, slope = 0.f, m = -INFINITY, l = 0.f;
+    const PT* pq_row = nullptr;
+    f32x4 o[NV];
 
     for (;;) {
-        const int h = seg.grp / p.row_tiles, r0 = (seg.grp - h * p.row_tiles) * kPaRows;
-        const int rows = min(kPaRows, rows_all - r0), len = seg.len;
-        const int start = p.starts ? min(max(const_ints(p.starts)[seg.b], -(1 << 30)), 1 << 30) : len - p.N;
-        const long long row_base = (long long)seg.b * p.H * p.N + (long long)h * rows_all + r0;      // of q, out, lse
-
-        // the lane's query row
-        const bool has_row = i < rows;
-        const int pos = start + (r0 + i) % p.N;
-        const int limit = !has_row ? 0 : (p.causal ? (pos >= len || pos < 0 ? 0 : pos + 1) : len);      // keys the row sees
-        const int all_see = p.causal ? max(min(start + 1, len), 0) : len;                               // keys every row sees
-        typename S::Query q;
+        f32x4 sc[GROUPS];
+        int held = 0;
+        bool whole = false;
+        if (have) {
+            if (k0 == s.t0 * KW + (SPLIT ? 0 : wave * KW)) {
+                // ---- a segment begins ----
+                h = p.row_tiles == 1 ? s.grp : s.grp / p.row_tiles;
+                const int r0 = (s.grp - h * p.row_tiles) * kPaRows;
+                rows = min(kPaRows, rows_all - r0);
+                row_base = (long long)s.b * p.H * p.N + (long long)h * rows_all + r0;       // of q, out, lse
+                has_row = i < rows;
+                // (r0 + i) / N and the rest, rows below 2^24
+                int head = (int)((float)(r0 + i) * p.inv_n);
+                int n = r0 + i - head * p.N;
+                if (n < 0) head--, n += p.N;
+                else if (n >= p.N) head++, n -= p.N;
+                pos = s.start + n;
+                limit = !has_row ? 0 : (p.causal ? (pos >= s.len || pos < 0 ? 0 : pos + 1) : s.len);     // keys the row sees
+                all_see = p.causal ? max(min(s.start + 1, s.len), 0) : s.len;                           // keys every row sees
 #pragma unroll
-        for (int x = 0; x < S::NU; x++) {
-            q.x[x] = {};
-            if (has_row) q.x[x] = S::row_chunk((const T*)p.q + (row_base + i) * C, g, x);
-        }
-        float phi_q[4] = {0.f, 0.f, 0.f, 0.f};
-        const PT* pq_row = nullptr;
-        if constexpr (NF > 0) {
-            pq_row = (const PT*)p.phi_q + (long long)seg.b * p.phiq_bstride + ((long long)h * rows_all + r0 + i) * p.R;
-#pragma unroll
-            for (int x = 0; x < NF; x++)
-                if (has_row && NF * g + x < p.R) phi_q[x] = (float)pq_row[NF * g + x];
-        }
-        float slope = 0.f;
-        if constexpr (BIAS == kBiasAlibi)
-            if (has_row) slope = p.slopes[h * (p.H / p.Hkv) + (r0 + i) / p.N];
-
-        Segment after = seg;                              // the worker's next segment
-        const bool has_after = SPLIT && left > 0;
-        if constexpr (SPLIT) {
-            if (has_after) {
-                after.grp++;
-                if (after.grp == groups) {
-                    after.grp = 0;
-                    after.b++;
-                    after.len = held_keys(p, after.b);
-                    after.n_steps = steps_of<KW>(after.len);
+                for (int x = 0; x < S::NU; x++) {
+                    q.x[x] = {};
+                    if (has_row) q.x[x] = S::row_chunk((const T*)p.q + (row_base + i) * C, g, x);
                 }
-                after.t0 = 0;
-                after.t1 = (int)min((long long)after.n_steps, left);
-                left -= after.t1;
-            }
-        }
-
-        float m = -INFINITY, l = 0.f;
-        f32x4 o[NV];
-#pragma unroll
-        for (int t = 0; t < NV; t++) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-        const int k_end = key_end(seg);
-        int k0 = first_key(seg);                          // wave-uniform
-        const auto next_pages = [&](int k) __attribute__((always_inline)) {       // of the step behind the one at k - STRIDE
-            if (k < k_end) pages_at(page, seg, k, k_end);
-            else if (has_after) pages_at(page, after, first_key(after), key_end(after));
-        };
-        const bool idle = k0 >= k_end;                    // no keys at all: the next segment's first step is still to be loaded
-        next_pages(k0 + STRIDE);
-        if (idle && has_after) {
-            rows_of(row, page, after.grp / p.row_tiles, 0);
-            if (key_end(after) > 0) {
-                load_keys(row);
-                load_values(row);
-            }
-        }
-        for (; k0 < k_end; k0 += STRIDE) {
-            const bool more = k0 + STRIDE < k_end, load = more || (has_after && key_end(after) > 0);
-            if (more) rows_of(next, page, h, k0 + STRIDE);
-            else rows_of(next, page, after.grp / p.row_tiles, first_key(after));
-            if (more) next_pages(k0 + 2 * STRIDE);
-            bool whole = k0 + KW <= all_see;
-#pragma unroll
-            for (int s = 0; s < GROUPS; s++) whole = whole && row[s] >= 0;
-            f32x4 sc[GROUPS];
-#pragma unroll
-            for (int s = 0; s < GROUPS; s++) {
-                sc[s] = S::scores(kr, s, q);
-                const int key0 = k0 + 16 * s + 4 * g;
                 if constexpr (NF > 0) {
-                    f32x4 f = {0.f, 0.f, 0.f, 0.f};
+                    pq_row = (const PT*)p.phi_q + (long long)s.b * p.phiq_bstride + ((long long)h * rows_all + r0 + i) * p.R;
 #pragma unroll
-                    for (int x = 0; x < NF; x++) f = __builtin_amdgcn_mfma_f32_16x16x4f32((float)fr[s][x], phi_q[x], f, 0, 0, 0);
+                    for (int x = 0; x < NF; x++) {
+                        phi_q[x] = 0.f;
+                        if (has_row && NF * g + x < p.R) phi_q[x] = (float)pq_row[NF * g + x];
+                    }
+                }
+                if constexpr (BIAS == kBiasAlibi)
+                    if (has_row) slope = p.slopes[h * p.G + head];
+                m = -INFINITY;
+                l = 0.f;
+#pragma unroll
+                for (int t = 0; t < NV; t++) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int x = 0; x < GROUPS; x++) held |= page[x] >= 0 ? 1 << x : 0;
+            whole = k0 + KW <= all_see && held == (1 << GROUPS) - 1;
+#pragma unroll
+            for (int x = 0; x < GROUPS; x++) {
+                sc[x] = S::scores(kr, x, q);
+                const int key0 = k0 + 16 * x + 4 * g;
+                if constexpr (NF > 0) {
+                    f32x4 b = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int y = 0; y < NF; y++) b = __builtin_amdgcn_mfma_f32_16x16x4f32(factor(fr[x], y), phi_q[y], b, 0, 0, 0);
                     if constexpr (BIAS == kBiasFactors) {
-                        const PT* pk = (const PT*)p.phi_pages + ((row[s] >= 0 ? row[s] : 0) + i) * p.R;
-                        for (int x = 4; 4 * x < p.R; x++) {
-                            const bool in = 4 * x + g < p.R;
-                            const float a = in ? (float)pk[4 * x + g] : 0.f, c = in && has_row ? (float)pq_row[4 * x + g] : 0.f;
-                            f = __builtin_amdgcn_mfma_f32_16x16x4f32(a, c, f, 0, 0, 0);
+                        const PT* pk = (const PT*)p.phi_pages + (row_at(page[x], h, k0 + 16 * x) + i) * p.R;
+                        for (int y = 4; 4 * y < p.R; y++) {
+                            const bool in = 4 * y + g < p.R;
+                            const float a = in ? (float)pk[4 * y + g] : 0.f, c = in && has_row ? (float)pq_row[4 * y + g] : 0.f;
+                            b = __builtin_amdgcn_mfma_f32_16x16x4f32(a, c, b, 0, 0, 0);
                         }
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; r++) sc[s][r] = fmaf(sc[s][r], p.scale, f[r]);
+                    for (int r = 0; r < 4; r++) sc[x][r] = fmaf(sc[x][r], p.scale, b[r]);
                 } else {
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        sc[s][r] *= p.scale;
-                        if constexpr (BIAS == kBiasAlibi) sc[s][r] = fmaf(slope, (float)(key0 + r - pos), sc[s][r]);
+                        sc[x][r] *= p.scale;
+                        if constexpr (BIAS == kBiasAlibi) sc[x][r] = fmaf(slope, (float)(key0 + r - pos), sc[x][r]);
                     }
                 }
                 if (!whole) {
 #pragma unroll
                     for (int r = 0; r < 4; r++)
-                        if (key0 + r >= limit || row[s] < 0) sc[s][r] = -INFINITY;
+                        if (key0 + r >= limit || !(held >> x & 1)) sc[x][r] = -INFINITY;
                 }
             }
-            if (load) load_keys(next);
+        }
+        const int fh = p.row_tiles == 1 ? f.grp : f.grp / p.row_tiles;
+        if (more) {
+#pragma unroll
+            for (int x = 0; x < GROUPS; x++) {
+                const long long at = row_at(f_page[x], fh, fk + 16 * x);
+                S::load_keys(kr, x, (const T*)p.k_pages + at * C, g, i);
+                if constexpr (NF > 0) load_factors(fr[x], (const PT*)p.phi_pages + (at + i) * p.R);
+            }
+        }
+        if (have) {
             // ---- softmax of the rows ----
             float mx = m;
 #pragma unroll
-            for (int s = 0; s < GROUPS; s++)
+            for (int x = 0; x < GROUPS; x++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[s][r]);
+                for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[x][r]);
             mx = column_max(mx);
             if (__any(mx > m)) {
                 const float alpha = weight(m, mx);
@@ -504,53 +519,57 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
             }
             const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-            for (int s = 0; s < GROUPS; s++)
+            for (int x = 0; x < GROUPS; x++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    sc[s][r] = fast_exp2((sc[s][r] - ref) * kLog2e);
-                    l += sc[s][r];
+                    sc[x][r] = fast_exp2((sc[x][r] - ref) * kLog2e);
+                    l += sc[x][r];
                 }
             const typename S::Probs pr = S::probs(sc);
             // ---- values ----
-            if (whole) {
+            // Values a row does not see may be anything (0 * inf is NaN), so around the last keys rows of different limits are
+            // done one limit after the other, the largest first, with the values behind it cleared.
+            unsigned long long todo = whole ? ~0ull : __ballot(limit > k0);
+            bool mine = true;
+            while (todo != 0) {
+                if (whole) {
+                    todo = 0;
+                } else {
+                    const int sees = min(limit, k0 + KW);
+                    int cut = todo >> lane & 1 ? sees : 0;
 #pragma unroll
-                for (int t = 0; t < NV; t++) o[t] = S::product(vr, t, pr, o[t]);
-            } else {
-                // Values a row does not see may be anything (0 * inf is NaN), so rows of different limits are done one
-                // after the other with the values behind their limit cleared; at most N of them, only around the last keys.
-                unsigned long long todo = __ballot(limit > k0);
-                while (todo != 0) {
-                    const int cut = min(__builtin_amdgcn_readlane(limit, __builtin_ctzll(todo)), k0 + KW);
-                    const bool mine = min(limit, k0 + KW) == cut;
-                    typename S::Values vm = vr;
+                    for (int d = 1; d < 16; d *= 2) cut = max(cut, __shfl_xor(cut, d));
+                    mine = sees == cut;
+                    todo &= ~__ballot(mine);
 #pragma unroll
-                    for (int s = 0; s < GROUPS; s++)
+                    for (int x = 0; x < GROUPS; x++)
 #pragma unroll
                         for (int r = 0; r < 4; r++)
-                            if (k0 + 16 * s + 4 * g + r >= cut || row[s] < 0) vm.x[s][r] = {};
+                            if (k0 + 16 * x + 4 * g + r >= cut || !(held >> x & 1)) vr.x[x][r] = {};
+                }
 #pragma unroll
-                    for (int t = 0; t < NV; t++) {
-                        const f32x4 d = S::product(vm, t, pr, o[t]);
+                for (int t = 0; t < NV; t++) {
+                    const f32x4 d = S::product(vr, t, pr, o[t]);
 #pragma unroll
-                        for (int r = 0; r < 4; r++) o[t][r] = mine ? d[r] : o[t][r];
-                    }
-                    todo &= ~__ballot(mine);
+                    for (int r = 0; r < 4; r++) o[t][r] = mine ? d[r] : o[t][r];
                 }
             }
-            if (load) load_values(next);
+        }
+        if (more) {
 #pragma unroll
-            for (int s = 0; s < GROUPS; s++) row[s] = next[s];
+            for (int x = 0; x < GROUPS; x++) S::load_values(vr, x, (const T*)p.v_pages + row_at(f_page[x], fh, fk + 16 * x) * C, g, i);
         }
-
-        l = column_sum(l);
-        if (limit <= 0) {                                 // a row that sees nothing went along with the others
-            m = -INFINITY;
-            l = 0.f;
-        }
-        if constexpr (SPLIT) {
-            // The lane's channels of row i: 4 NV adjacent ones from 4 g NV on.
-            if (seg.t0 == 0 && seg.t1 == seg.n_steps) {
-                if (has_row) {
+        if (have && k0 + STRIDE >= min(s.len, s.t1 * KW)) {
+            // ---- a segment ends ----
+            l = column_sum(l);
+            if (limit <= 0) {                             // a row that sees nothing went along with the others
+                m = -INFINITY;
+                l = 0.f;
+            }
+            if constexpr (SPLIT) {
+                // The lane's channels of row i: 4 NV adjacent ones from 4 g NV on.
+                const bool all = s.t0 == 0 && s.t1 == s.n_steps;
+                if (all && has_row) {
                     const float inv = l == 0.f ? 0.f : 1.f / l;
                     struct alignas(4 * NV * sizeof(T) < 16 ? 4 * NV * sizeof(T) : 16) Mine { T x[4 * NV]; } v;
 #pragma unroll
@@ -560,72 +579,88 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
                     *(Mine*)((T*)p.out + (row_base + i) * C + 4 * g * NV) = v;
                     if (g == 0) p.lse[row_base + i] = l == 0.f ? -INFINITY : m + __log2f(l) * kLn2;
                 }
-            } else if (has_row) {
-                const long long at = ((long long)worker * 2 + (seg.t0 > 0 ? 0 : 1)) * part_rows + i;
-                struct alignas(16) Mine { float x[4 * NV]; } v;
+                if (!all && has_row) {
+                    const long long at = ((long long)worker * 2 + (s.t0 > 0 ? 0 : 1)) * min(kPaRows, rows_all) + i;
+                    struct alignas(16) Mine { float x[4 * NV]; } v;
 #pragma unroll
-                for (int r = 0; r < 4; r++)
+                    for (int r = 0; r < 4; r++)
 #pragma unroll
-                    for (int t = 0; t < NV; t++) v.x[r * NV + t] = o[t][r];
-                *(Mine*)(p.part_o + at * C + 4 * g * NV) = v;
-                if (g == 0) {
-                    p.part_m[at] = m;
-                    p.part_l[at] = l;
+                        for (int t = 0; t < NV; t++) v.x[r * NV + t] = o[t][r];
+                    *(Mine*)(p.part_o + at * C + 4 * g * NV) = v;
+                    if (g == 0) {
+                        p.part_m[at] = m;
+                        p.part_l[at] = l;
+                    }
+                }
+                // The group's first worker says who has the rest; a share that ends inside a group ends with its step t1.
+                if (lane == 0) {
+                    int rest = 0;
+                    if (s.t0 == 0 && s.t1 < s.n_steps) rest = share.worker_of(share.u_end - 1 + s.n_steps - s.t1) - worker;
+                    const int4 join = make_int4(rest, worker, s.b * groups + s.grp, rows);
+                    if (p.joins_by_group) {
+                        if (s.t0 == 0) p.joins[join.z] = join;
+                    } else if (!more) {
+                        p.joins[worker] = join;
+                    }
+                }
+            } else {
+                // ---- the waves of the workgroup ----
+                __shared__ __align__(16) float sm_o[kPaWaves][kPaRows][C + 4];      // + 4: rows start in different banks
+                __shared__ float sm_m[kPaWaves][kPaRows], sm_l[kPaWaves][kPaRows];
+                if (has_row) {
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+#pragma unroll
+                        for (int t = 0; t < NV; t++) sm_o[wave][i][(4 * g + r) * NV + t] = o[t][r];
+                    if (g == 0) {
+                        sm_m[wave][i] = m;
+                        sm_l[wave][i] = l;
+                    }
+                }
+                __syncthreads();
+                for (int x = tid; x < rows * (C / 4); x += kPaThreads) {
+                    const int r = x / (C / 4), c4 = x % (C / 4);
+                    float mx = sm_m[0][r];
+#pragma unroll
+                    for (int w = 1; w < kPaWaves; w++) mx = fmaxf(mx, sm_m[w][r]);
+                    float lt = 0.f;
+                    f32x4 ot = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int w = 0; w < kPaWaves; w++) {
+                        const float a = weight(sm_m[w][r], mx);
+                        const f32x4 y = *(const f32x4*)&sm_o[w][r][c4 * 4];
+                        lt = fmaf(a, sm_l[w][r], lt);
+#pragma unroll
+                        for (int e = 0; e < 4; e++) ot[e] = fmaf(a, y[e], ot[e]);
+                    }
+                    write_row<T, C>(p, row_base + r, c4, ot, lt, mx);
                 }
             }
-            if (seg.t0 == 0) {                            // the group's first worker says who has the rest
-                int more = 0;
-                if (seg.t1 < seg.n_steps) {
-                    // the group's last step is share.u_end - 1 + (n_steps - t1): here the share ends inside the group
-                    const long long last = share.u_end - 1 + (seg.n_steps - seg.t1);
-                    more = (int)(((last + 1) * share.workers - 1) / share.total) - worker;
-                }
-                const int4 mine = make_int4(more, worker, (int)((long long)seg.b * groups + seg.grp), rows);
-                if (p.joins_by_group) {
-                    if (lane == 0) p.joins[mine.z] = mine;
-                } else if (more > 0) {
-                    join = mine;
-                }
-            }
-            if (!has_after) break;
-            seg = after;
-        } else {
-            // ---- the waves of the workgroup ----
-            __shared__ __align__(16) float sm_o[kPaWaves][kPaRows][C + 4];      // + 4: rows start in different banks
-            __shared__ float sm_m[kPaWaves][kPaRows], sm_l[kPaWaves][kPaRows];
-            if (has_row) {
-#pragma unroll
-                for (int r = 0; r < 4; r++)
-#pragma unroll
-                    for (int t = 0; t < NV; t++) sm_o[wave][i][(4 * g + r) * NV + t] = o[t][r];
-                if (g == 0) {
-                    sm_m[wave][i] = m;
-                    sm_l[wave][i] = l;
-                }
-            }
-            __syncthreads();
-            for (int x = tid; x < rows * (C / 4); x += kPaThreads) {
-                const int r = x / (C / 4), c4 = x % (C / 4);
-                float mx = sm_m[0][r];
-#pragma unroll
-                for (int w = 1; w < kPaWaves; w++) mx = fmaxf(mx, sm_m[w][r]);
-                float lt = 0.f;
-                f32x4 ot = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int w = 0; w < kPaWaves; w++) {
-                    const float a = weight(sm_m[w][r], mx);
-                    const f32x4 y = *(const f32x4*)&sm_o[w][r][c4 * 4];
-                    lt = fmaf(a, sm_l[w][r], lt);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) ot[e] = fmaf(a, y[e], ot[e]);
-                }
-                write_row<T, C>(p, row_base + r, c4, ot, lt, mx);
-            }
-            break;
         }
+        if (!more) return;
+        // ---- on to the step that was just loaded, and the one behind it ----
+        s = f;
+        k0 = fk;
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) page[x] = f_page[x];
+        have = true;
+        if (fk + STRIDE < min(f.len, f.t1 * KW)) {
+            fk += STRIDE;
+        } else if (SPLIT && left > kPaLead) {
+            if (++f.grp == groups) {
+                f.grp = 0;
+                f.b++;
+                enter(f);
+            }
+            f.t0 = 0;
+            f.t1 = min(f.n_steps, left - kPaLead);
+            left -= f.t1 + kPaLead;
+            fk = 0;
+        } else {
+            more = false;
+        }
+        if (more) pages_at(f_page, f, fk);
     }
-    if constexpr (SPLIT)
-        if (!p.joins_by_group && lane == 0) p.joins[worker] = join;
 }
 
 // Joins the parts of a group's rows: part 1 of the worker where the group begins and part 0 of the `more` workers behind
@@ -641,7 +676,7 @@ __global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, in
     const int r = blockIdx.y * (SL / lanes) + slot / lanes;
     if (more == 0) return;                                // (uniform)
     const bool has_row = r < join.w;
-    const int part_rows = min(kPaRows, p.H / p.Hkv * p.N);
+    const int part_rows = min(kPaRows, p.G * p.N);
     auto part = [&](int k) { return ((long long)(first + k) * 2 + (k == 0 ? 1 : 0)) * part_rows + (has_row ? r : 0); };
 
     // the slot's parts, and then the slots', each by the running maximum
@@ -694,7 +729,7 @@ __global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, in
     }
     const int b = join.z / (p.Hkv * p.row_tiles), grp = join.z - b * p.Hkv * p.row_tiles;
     const int h = grp / p.row_tiles, r0 = (grp - h * p.row_tiles) * kPaRows;
-    write_row<T, C>(p, (long long)b * p.H * p.N + (long long)h * (p.H / p.Hkv * p.N) + r0 + r, c4, ot, lt, mx);
+    write_row<T, C>(p, (long long)b * p.H * p.N + (long long)h * (p.G * p.N) + r0 + r, c4, ot, lt, mx);
 }
 
 template <typename T, int C, int BIAS, bool PF32>
@@ -709,7 +744,7 @@ int launch_attn(const PagedAttnParams& p, hipStream_t stream) {
                        stream, p);
     if (hipGetLastError() != hipSuccess) return 1;
     const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
-    const int rows = p.H / p.Hkv * p.N < kPaRows ? p.H / p.Hkv * p.N : kPaRows;
+    const int rows = p.G * p.N < kPaRows ? p.G * p.N : kPaRows;
     // slots: as many parts at a time as a group has on average, the rest are rows
     const long long parts = p.workers / groups;
     const int lanes = parts >= 6 ? 8 : (parts >= 3 ? 4 : 2);
@@ -718,14 +753,21 @@ int launch_attn(const PagedAttnParams& p, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
+template <typename T, int C, bool PF32>
+int attn_factors(const PagedAttnParams& p, hipStream_t stream) {
+    if (p.R <= 4) return launch_attn<T, C, kBiasFactors4, PF32>(p, stream);
+    if (p.R <= 16 && p.R % 4 == 0) return launch_attn<T, C, kBiasFactors16, PF32>(p, stream);
+    return launch_attn<T, C, kBiasFactors, PF32>(p, stream);
+}
+
 template <typename T, int C>
 int attn_bias(const PagedAttnParams& p, hipStream_t stream) {
     if (p.slopes) return launch_attn<T, C, kBiasAlibi, true>(p, stream);
     if (p.R == 0) return launch_attn<T, C, kBiasNone, true>(p, stream);
     if constexpr (!std::is_same_v<T, float>) {
-        if (!p.phi_f32) return p.R <= 4 ? launch_attn<T, C, kBiasFactors4, false>(p, stream) : launch_attn<T, C, kBiasFactors, false>(p, stream);
+        if (!p.phi_f32) return attn_factors<T, C, false>(p, stream);
     }
-    return p.R <= 4 ? launch_attn<T, C, kBiasFactors4, true>(p, stream) : launch_attn<T, C, kBiasFactors, true>(p, stream);
+    return attn_factors<T, C, true>(p, stream);
 }
 
 template <typename T>
@@ -741,15 +783,15 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 
 }  // namespace
 
-// Waves that share the keys: all that are resident, two per SIMD.  Requests of at most 16 steps are not split.
+// Waves that share the keys: all that are resident, two per SIMD.  Requests of at most 512 keys are not split.
 int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32) {
-    const int step = f32 ? 16 : 32;
+    const int step = 16 * (f32 ? PA_GF(C) : PA_GB(C));               // Step::KW
     const long long steps = (capacity + step - 1) / step;
-    if (steps <= 16) return 0;
+    if (capacity <= PA_DIRECT) return 0;
     int cus = fb_cu_count();
     if (cus <= 0) cus = 256;
     const long long groups = (long long)B * Hkv * row_tiles;
-    if (steps * Hkv * row_tiles >= (1LL << 31)) return 0;            // a request's steps are counted in 32 bits
+    if ((steps + kPaLead) * groups >= (1LL << 31)) return 0;         // costs are counted in 32 bits
     const long long most = groups * ((steps + kPaLeast - 1) / kPaLeast), all = 8LL * cus;
     return (int)(most < all ? most : all);
 }
@@ -762,9 +804,13 @@ size_t fb_paged_attn_workspace_bytes(int workers, long long groups, long long ro
 }
 
 int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream_t stream) {
+    p.G = p.H / p.Hkv;
+    p.inv_n = 1.0f / (float)p.N;
+    const long long capacity = (long long)p.max_blocks << p.page_shift;
+    p.capacity = capacity < 0x7fffff00 ? (int)capacity : 0x7fffff00;
     if (p.workers) {
         const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
-        const size_t parts = parts_of(p.workers, (long long)(p.H / p.Hkv) * p.N);
+        const size_t parts = parts_of(p.workers, (long long)p.G * p.N);
         p.joins_by_group = groups <= p.workers;
         p.joins = (int4*)ws;
         p.part_o = (float*)(p.joins + (p.joins_by_group ? groups : p.workers));

@@ -122,7 +122,9 @@ struct PagedAttnParams {
     long long phiq_bstride;
     int B, H, Hkv, N, R, page_shift, n_pages, max_blocks, causal, phi_f32;
     float scale;
-    int row_tiles;           // query rows of a key head (H / Hkv * N of them) in tiles of 16
+    int row_tiles;           // query rows of a key head (H / Hkv * N of them, below 2^24) in tiles of 16
+    int G, capacity;         // set by the launch: H / Hkv; keys that a table row has room for
+    float inv_n;             // 1 / N
     int workers;             // waves the keys are split over; 0: a workgroup per key head and row tile, no split
     int joins_by_group;      // joins has an entry per (request, key head, row tile), else one per worker
     float* part_o;           // scratch: two parts per worker, [workers, 2, rows, C], rows = min(16, H / Hkv * N)
