@@ -31,23 +31,8 @@ namespace {
 constexpr int kPaWaves = 4;
 constexpr int kPaThreads = kPaWaves * 64;
 constexpr int kPaRows = 16;
-#ifndef PA_DIRECT
-#define PA_DIRECT 512
-#endif
-#ifndef PA_LEAST
-#define PA_LEAST 2
-#endif
-#ifndef PA_GB
-#define PA_GB(C) 2
-#endif
-#ifndef PA_GF
-#define PA_GF(C) 1
-#endif
-constexpr int kPaLeast = PA_LEAST;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
-#ifndef PA_LEAD
-#define PA_LEAD 2
-#endif
-constexpr int kPaLead = PA_LEAD;        // steps that a group's beginning and end cost, counted into the shares
+constexpr int kPaLeast = 2;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
+constexpr int kPaLead = 2;        // steps that a group's beginning and end cost, counted into the shares
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
@@ -76,12 +61,14 @@ FB_DEV float weight(float a, float m) { return a == -INFINITY ? 0.f : fast_exp2(
 // KW: as many as 64 registers of keys and values hold, up to 64 (a wave has one step in flight, and a step takes a
 // memory latency at least: 32 keys a step at 64 channels are slower).
 // Lane l: g = l / 16, i = l % 16.  S^T group s (16 keys): column i (the query row), keys 4 g + r.
-template <typename T, int C>
+template <typename T, int C, int GROUPS>
 struct Step;
+constexpr int step_groups(int c, bool f32) { return (c <= 32 ? 4 : 2) / (f32 ? 2 : 1); }
+constexpr int waves_per_simd(int c) { return c == 16 ? 4 : 2; }
 
-template <int C>
-struct Step<bf16_t, C> {
-    static constexpr int GROUPS = PA_GB(C), KW = 16 * GROUPS, NV = C / 16;
+template <int C, int GROUPS>
+struct Step<bf16_t, C, GROUPS> {
+    static constexpr int KW = 16 * GROUPS, NV = C / 16;
     static constexpr int NU = C >= 32 ? C / 32 : 1;
     using KVec = std::conditional_t<C == 16, u32x2, u32x4>;
     using VVec = std::conditional_t<NV == 8, u32x4, std::conditional_t<NV == 4, u32x2, std::conditional_t<NV == 2, unsigned, unsigned short>>>;
@@ -144,9 +131,9 @@ struct Step<bf16_t, C> {
     }
 };
 
-template <int C>
-struct Step<float, C> {
-    static constexpr int GROUPS = PA_GF(C), KW = 16 * GROUPS, NV = C / 16;
+template <int C, int GROUPS>
+struct Step<float, C, GROUPS> {
+    static constexpr int KW = 16 * GROUPS, NV = C / 16;
     static constexpr int NU = C / 16;
     using VVec = std::conditional_t<NV == 8, f32x8, std::conditional_t<NV == 4, f32x4, std::conditional_t<NV == 2, f32x2, float>>>;
     struct Query { f32x4 x[NU]; };
@@ -222,6 +209,7 @@ FB_DEV int wave_scan(int x) {
 // All below 2^31 (the launch sees to it).
 struct Share {
     int u, u_end, b, rem;
+    int len, start;          // of request b, as stored
     int base, longer, workers;
     FB_DEV void cut(int total, int most, int worker) {
         workers = min(most, (total + kPaLeast - 1) / kPaLeast);
@@ -241,19 +229,22 @@ FB_DEV Share share_of(const PagedAttnParams& p, int groups, int worker) {
     __shared__ int sm_sum[kPaWaves], sm_b[kPaWaves], sm_rem[kPaWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Share s{};
-    const auto cost = [&](int b) { return b < p.B ? (steps_of<KW>(held_keys(p, p.lens[b])) + kPaLead) * groups : 0; };
+    const auto cost = [&](int b, int len) { return b < p.B ? (steps_of<KW>(held_keys(p, len)) + kPaLead) * groups : 0; };
     if (p.B <= 64) {                                     // every wave by itself
-        const int own = cost(lane), end = wave_scan(own);
+        const int at = min(lane, p.B - 1), len = p.lens[at], start = p.starts ? p.starts[at] : 0;
+        const int own = cost(lane, len), end = wave_scan(own);
         s.cut(__builtin_amdgcn_readlane(end, 63), p.workers, worker);
         if (s.u < s.u_end) {
             s.b = __builtin_ctzll(__ballot(end > s.u));
             s.rem = s.u - __builtin_amdgcn_readlane(end - own, s.b);
+            s.len = __builtin_amdgcn_readlane(len, s.b);
+            s.start = __builtin_amdgcn_readlane(start, s.b);
         }
         return s;
     }
     // the workgroup's four shares together, 256 requests at a time: the total first
     const auto tile = [&](int b0, int& own, int& sum) {
-        own = cost(b0 + tid);
+        own = cost(b0 + tid, p.lens[min(b0 + tid, p.B - 1)]);
         const int in_wave = wave_scan(own);
         __syncthreads();
         if (lane == 63) sm_sum[wave] = in_wave;
@@ -285,8 +276,12 @@ FB_DEV Share share_of(const PagedAttnParams& p, int groups, int worker) {
         before += sum;
     }
     __syncthreads();
-    s.b = sm_b[wave];                                    // (waves without a share do not read on)
-    s.rem = sm_rem[wave];
+    if (s.u < s.u_end) {
+        s.b = __builtin_amdgcn_readfirstlane(sm_b[wave]);
+        s.rem = sm_rem[wave];
+        s.len = const_ints(p.lens)[s.b];
+        s.start = p.starts ? const_ints(p.starts)[s.b] : 0;
+    }
     return s;
 }
 
@@ -308,9 +303,10 @@ struct Segment {
 
 // BIAS, PF32: kind of bias and whether the factors are float
 template <typename T, int C, int BIAS, bool PF32, bool SPLIT>
-__global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnParams p) {
-    using S = Step<T, C>;
-    constexpr int KW = S::KW, NV = S::NV, GROUPS = S::GROUPS;
+__global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kernel(PagedAttnParams p) {
+    constexpr int GROUPS = step_groups(C, std::is_same_v<T, float>);
+    using S = Step<T, C, GROUPS>;
+    constexpr int KW = S::KW, NV = S::NV;
     constexpr int STRIDE = SPLIT ? KW : kPaWaves * KW;    // keys from one step of a wave to its next
     constexpr int NF = BIAS == kBiasFactors4 ? 1 : (BIAS >= kBiasFactors16 ? 4 : 0);
     using PT = std::conditional_t<PF32, float, bf16_t>;
@@ -322,10 +318,13 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
     const int rows_all = p.G * p.N;
     const int page_mask = (1 << p.page_shift) - 1;
 
-    auto enter = [&](Segment& s) __attribute__((always_inline)) {          // request s.b
-        s.len = held_keys(p, const_ints(p.lens)[s.b]);
+    auto enter = [&](Segment& s, int len, int start) __attribute__((always_inline)) {      // request s.b, its len and start as stored
+        s.len = held_keys(p, len);
         s.n_steps = steps_of<KW>(s.len);
-        s.start = p.starts ? min(max(const_ints(p.starts)[s.b], -(1 << 30)), 1 << 30) : s.len - p.N;
+        s.start = p.starts ? min(max(start, -(1 << 30)), 1 << 30) : s.len - p.N;
+    };
+    auto enter_next = [&](Segment& s) __attribute__((always_inline)) {
+        enter(s, const_ints(p.lens)[s.b], p.starts ? const_ints(p.starts)[s.b] : 0);
     };
     Segment f;                                            // of the step to load next, at key fk
     Share share{};
@@ -337,7 +336,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
         left = __builtin_amdgcn_readfirstlane(share.u_end - share.u);
         f.t0 = f.t1 = 0;
         if (left > 0) {
-            enter(f);
+            enter(f, __builtin_amdgcn_readfirstlane(share.len), __builtin_amdgcn_readfirstlane(share.start));
             const int rem = __builtin_amdgcn_readfirstlane(share.rem), cost = f.n_steps + kPaLead;
             f.grp = __builtin_amdgcn_readfirstlane((int)((unsigned)rem / (unsigned)cost));
             const int at = rem - f.grp * cost;            // the share's beginning in the group's costs
@@ -352,7 +351,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
     } else {
         f.b = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)groups);
         f.grp = blockIdx.x - f.b * groups;
-        enter(f);
+        enter_next(f);
         f.t0 = 0;
         f.t1 = f.n_steps;
     }
@@ -650,7 +649,7 @@ __global__ __launch_bounds__(kPaThreads, 2) void paged_attn_kernel(PagedAttnPara
             if (++f.grp == groups) {
                 f.grp = 0;
                 f.b++;
-                enter(f);
+                enter_next(f);
             }
             f.t0 = 0;
             f.t1 = min(f.n_steps, left - kPaLead);
@@ -785,14 +784,14 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 
 // Waves that share the keys: all that are resident, two per SIMD.  Requests of at most 512 keys are not split.
 int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32) {
-    const int step = 16 * (f32 ? PA_GF(C) : PA_GB(C));               // Step::KW
+    const int step = 16 * step_groups(C, f32);
     const long long steps = (capacity + step - 1) / step;
-    if (capacity <= PA_DIRECT) return 0;
+    if (capacity <= (f32 ? 320 : 640)) return 0;
     int cus = fb_cu_count();
     if (cus <= 0) cus = 256;
     const long long groups = (long long)B * Hkv * row_tiles;
     if ((steps + kPaLead) * groups >= (1LL << 31)) return 0;         // costs are counted in 32 bits
-    const long long most = groups * ((steps + kPaLeast - 1) / kPaLeast), all = 8LL * cus;
+    const long long most = groups * ((steps + kPaLeast - 1) / kPaLeast), all = 4LL * waves_per_simd(C) * cus;
     return (int)(most < all ? most : all);
 }
 
