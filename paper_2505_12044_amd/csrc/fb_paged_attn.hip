@@ -400,8 +400,8 @@ __global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kern
     };
 
     // One loop over the steps of all segments, one step ahead: the next step's keys are loaded when the scores have used this
-    // one's, its values after this one's product, its pages before that.  (The first turn only loads: the code is walked
-    // through cold by every CU, and a second copy of the loads costs more than it saves.)
+    // one's, its values after this one's product, its pages before that.  With SPLIT the first turn only loads (every CU walks
+    // through the code cold, and many waves start at once: a second copy of the loads costs more than it saves).
     Segment s = f;
     int fk = f.t0 * KW + (SPLIT ? 0 : wave * KW), k0 = 0;
     int f_page[GROUPS], page[GROUPS];
@@ -452,7 +452,49 @@ __global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kern
 #pragma unroll
         for (int t = 0; t < NV; t++) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
-    if constexpr (!SPLIT) begin();                        // there is one, and its query rows are the first to be read
+    auto load_keys = [&]() __attribute__((always_inline)) {              // of step f, fk
+        const int fh = p.row_tiles == 1 ? f.grp : f.grp / p.row_tiles;
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) {
+            const long long at = row_at(f_page[x], fh, fk + 16 * x);
+            S::load_keys(kr, x, (const T*)p.k_pages + at * C, g, i);
+            if constexpr (NF > 0) load_factors(fr[x], (const PT*)p.phi_pages + (at + i) * p.R);
+        }
+    };
+    auto load_values = [&]() __attribute__((always_inline)) {
+        const int fh = p.row_tiles == 1 ? f.grp : f.grp / p.row_tiles;
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) S::load_values(vr, x, (const T*)p.v_pages + row_at(f_page[x], fh, fk + 16 * x) * C, g, i);
+    };
+    auto advance = [&]() __attribute__((always_inline)) {               // on to the step that was just loaded, and the one behind it
+        s = f;
+        k0 = fk;
+#pragma unroll
+        for (int x = 0; x < GROUPS; x++) page[x] = f_page[x];
+        have = true;
+        if (fk + STRIDE < min(f.len, f.t1 * KW)) {
+            fk += STRIDE;
+        } else if (SPLIT && left > kPaLead) {
+            if (++f.grp == groups) {
+                f.grp = 0;
+                f.b++;
+                enter_next(f);
+            }
+            f.t0 = 0;
+            f.t1 = min(f.n_steps, left - kPaLead);
+            left -= f.t1 + kPaLead;
+            fk = 0;
+        } else {
+            more = false;
+        }
+        if (more) pages_at(f_page, f, fk);
+    };
+    if constexpr (!SPLIT) {       // one segment: its query rows are the first to be read
+        begin();
+        load_keys();
+        load_values();
+        advance();
+    }
 
     for (;;) {
         f32x4 sc[GROUPS];
@@ -496,15 +538,7 @@ __global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kern
                 }
             }
         }
-        const int fh = p.row_tiles == 1 ? f.grp : f.grp / p.row_tiles;
-        if (more) {
-#pragma unroll
-            for (int x = 0; x < GROUPS; x++) {
-                const long long at = row_at(f_page[x], fh, fk + 16 * x);
-                S::load_keys(kr, x, (const T*)p.k_pages + at * C, g, i);
-                if constexpr (NF > 0) load_factors(fr[x], (const PT*)p.phi_pages + (at + i) * p.R);
-            }
-        }
+        if (more) load_keys();
         if (have) {
             // ---- softmax of the rows ----
             float mx = m;
@@ -560,10 +594,7 @@ __global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kern
                 }
             }
         }
-        if (more) {
-#pragma unroll
-            for (int x = 0; x < GROUPS; x++) S::load_values(vr, x, (const T*)p.v_pages + row_at(f_page[x], fh, fk + 16 * x) * C, g, i);
-        }
+        if (more) load_values();
         if (have && k0 + STRIDE >= min(s.len, s.t1 * KW)) {
             // ---- a segment ends ----
             l = column_sum(l);
@@ -643,28 +674,7 @@ __global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kern
             }
         }
         if (!more) return;
-        // ---- on to the step that was just loaded, and the one behind it ----
-        s = f;
-        k0 = fk;
-#pragma unroll
-        for (int x = 0; x < GROUPS; x++) page[x] = f_page[x];
-        have = true;
-        if (fk + STRIDE < min(f.len, f.t1 * KW)) {
-            fk += STRIDE;
-        } else if (SPLIT && left > kPaLead) {
-            if (++f.grp == groups) {
-                f.grp = 0;
-                f.b++;
-                enter_next(f);
-            }
-            f.t0 = 0;
-            f.t1 = min(f.n_steps, left - kPaLead);
-            left -= f.t1 + kPaLead;
-            fk = 0;
-        } else {
-            more = false;
-        }
-        if (more) pages_at(f_page, f, fk);
+        advance();
     }
 }
 
