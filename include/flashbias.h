@@ -359,7 +359,7 @@ int fb_rotary_bwd(const void* dy0, void* dx0, int H0, const void* dy1, void* dx1
  *   then requests that grow take theirs from its head in the order of b: request b gets its pages if the pages that requests
  *   0..b need add up to no more than are free.  One that does not, one whose new length exceeds max_blocks * page, or that grows
  *   by more than N tokens, keeps its length; its slots are -1.  Negative lengths count as 0.
- *   lens_out [B], state_out [2]: lengths and free pages afterwards (not in place).  table and ring are updated in place;
+ *   lens_out [B], state_out [2]: lengths and free pages afterwards (not in place, no overlap with the inputs).  table and ring are updated in place;
  *   table entries behind a request's last page keep what they held.  slots [B, N]: slot of the request's i-th new token, -1
  *   behind the last; positions [B, N] or NULL: its position in the request, 0 behind the last.
  *   B <= 4096.  A page must be owned once: in the ring or by one request.  An entry that is no page gives slot -1.
@@ -381,12 +381,13 @@ int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* 
 /*
  * Attention of N new tokens per request over the pages (one in decode, a few when drafted tokens are checked): q, out
  * [B,H,N,C], lse [B,H,N]; query head h reads key head h / (H / Hkv).  Bias: factors phi_q [Bp,H,N,R] against phi_pages (R <= 64),
- * or ALiBi -slopes[h] (i - j) (slopes [H] float, R = 0), or none.
+ * or ALiBi -slopes[h] (i - j) (slopes [H] float, R = 0; exact below 2^24 positions), or none.
  *   Query n of request b has the position i = starts[b] + n (starts NULL: lens[b] - N + n).  causal: it sees the keys
  *   j <= i of the request and is no query at all when i lies outside [0, lens[b]); else it sees all lens[b] keys (states of an
  *   encoder).  Keys in a table entry that is no page are not seen; lens are cut to [0, max_blocks * page].  What lies in the pages behind the
  *   last token, or in rows a query does not see, never reaches the result.  A query that sees nothing, or scores of -infinity
  *   only, has out = 0 and lse = -infinity.
+ *   N is meant to be small: every 16 of a key head's H / Hkv * N query rows read its keys again (H / Hkv * N < 2^24).
  *   dtype FB_BF16 (products in bf16, probabilities in two bf16 limbs, everything else fp32) or FB_F32 (all fp32, fp32 factors).
  *   workspace: device scratch of fb_paged_attn_fwd_workspace_bytes(...) bytes, 16-byte aligned, contents ignored, for the parts
  *   of key heads that several workgroups share; without it (NULL, or too small) a key head stays in one workgroup.

@@ -508,14 +508,15 @@ def _need(ok: bool, what: str) -> None:
         raise FlashBiasError(what)
 
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """All tensors of a call live on the current device, whose stream the call goes to."""
+def _here(stream, *tensors: Optional[torch.Tensor]) -> Optional[int]:
+    """The stream's raw handle; all tensors of the call have to live on the current device, whose stream it is."""
     dev = tensors[0].get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise FlashBiasError("tensors must be CUDA tensors of the current device")
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise FlashBiasError("tensors must be CUDA tensors of the current device")
+    return torch._C._cuda_getCurrentRawStream(dev) or None if stream is None else _stream(stream)
 
 
 def _ints(name: str, t: torch.Tensor, *shape: int) -> int:
@@ -546,7 +547,7 @@ def _sections(sections: Tuple[int, ...]):
 
 def _rotary(lib_fn, what, x0, x1, positions, freqs, sections, interleaved, out, stream):
     strides = _row_strides(x0, x1)
-    _here(x0, x1, positions, freqs)
+    handle = _here(stream, x0, x1, positions, freqs)
     B, H0, N, C = x0.shape
     dtype = x0.dtype
     axes, pairs, c_sections = _sections(tuple(sections))
@@ -568,10 +569,10 @@ def _rotary(lib_fn, what, x0, x1, positions, freqs, sections, interleaved, out, 
         for x, y in ((x0, y0), (x1, y1)):
             _need((x is None) == (y is None) and (x is None or (y.shape == x.shape and y.dtype is dtype and y.is_contiguous())),
                   "outputs must be contiguous, with their inputs' shapes and dtype")
-        _here(y0, y1)
+        _here(stream, y0, y1)
     st = lib_fn(x0.data_ptr(), y0.data_ptr(), H0, None if x1 is None else x1.data_ptr(), None if y1 is None else y1.data_ptr(), H1,
                 strides, positions.data_ptr(), f32_pos, shape[1] == 1, freqs.data_ptr(), c_sections, B, N, C, bool(interleaved),
-                _dtype_code(x0), _stream(stream))
+                _dtype_code(x0), handle)
     _check(st, what)
     return y0, y1
 
@@ -596,7 +597,7 @@ def fb_paged_plan(lens, new_lens, table, ring, state, n_new: int, page: int, len
     free pages, int32, in place), and the up to n_new new tokens of each are mapped.  Returns lens [B] and state [2]
     (ring head, free pages) afterwards, slots [B, n_new] (-1: no token) and positions [B, n_new]."""
     lib = load_library()
-    _here(lens, new_lens, table, ring, state, lens_out, state_out, slots, positions)
+    handle = _here(stream, lens, new_lens, table, ring, state, lens_out, state_out, slots, positions)
     _need(lens.dim() == 1 and table.dim() == 2 and ring.dim() == 1, "lens, ring: one dimension, table: [B, max_blocks]")
     B, blocks, n_pages = lens.shape[0], table.shape[1], ring.shape[0]
     new = lens.new_empty
@@ -611,7 +612,7 @@ def fb_paged_plan(lens, new_lens, table, ring, state, n_new: int, page: int, len
     st = lib.fb_paged_plan(_ints("lens", lens, B), _ints("new_lens", new_lens, B), _ints("table", table, B, blocks),
                            _ints("ring", ring, n_pages), _ints("state", state, 2), _ints("lens_out", lens_out, B),
                            _ints("state_out", state_out, 2), _ints("slots", slots, B, n_new), _ints("positions", positions, B, n_new),
-                           B, n_new, page, n_pages, blocks, _stream(stream))
+                           B, n_new, page, n_pages, blocks, handle)
     _check(st, "fb_paged_plan")
     return lens_out, state_out, slots, positions
 
@@ -636,7 +637,7 @@ def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, p
     k_pages, v_pages [n_pages,Hkv,page,C] and phi_pages [n_pages,Hkv,page,R].  Slots of -1 are left out; the others must differ."""
     lib = load_library()
     strides = _row_strides(k, v)
-    _here(k, v, slots, k_pages, v_pages, phi_k, phi_pages)
+    handle = _here(stream, k, v, slots, k_pages, v_pages, phi_k, phi_pages)
     B, Hkv, N, C = k.shape
     n_pages, hp, page, cp, R = _check_pages(k_pages, v_pages, phi_pages, phi_k)
     _need(v.shape == k.shape and k.dtype is v.dtype and k.dtype is k_pages.dtype and hp == Hkv and cp == C,
@@ -649,7 +650,7 @@ def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, p
             phi_batch_broadcast = phi_k.shape[0] == 1 and B > 1
     st = lib.fb_paged_append(k.data_ptr(), v.data_ptr(), _ptr(phi_k), _ints("slots", slots, B, N), _ptr(k_pages), _ptr(v_pages),
                              _ptr(phi_pages), strides, B, Hkv, N, C, R, page, n_pages, code, phi_code,
-                             bool(phi_batch_broadcast), _stream(stream))
+                             bool(phi_batch_broadcast), handle)
     _check(st, "fb_paged_append")
 
 
@@ -673,7 +674,7 @@ def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None,
     fb_paged_attn_fwd_workspace_bytes: the caller's workspace, else the binding's own; a call that is given out and lse but no
     workspace allocates nothing and does without (a key head is then not split over the GPU)."""
     lib = load_library()
-    _here(q, k_pages, v_pages, table, lens, starts, phi_q, phi_pages, slopes, out, lse, workspace)
+    handle = _here(stream, q, k_pages, v_pages, table, lens, starts, phi_q, phi_pages, slopes, out, lse, workspace)
     _need(q.dim() == 4 and table.dim() == 2, "q must be [B,H,N,C], table [B, max_blocks]")
     B, H, N, C = q.shape
     blocks = table.shape[1]
@@ -705,6 +706,6 @@ def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None,
     st = lib.fb_paged_attn_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(phi_q), _ptr(phi_pages), _ptr(slopes),
                                _ints("table", table, B, blocks), _ints("lens", lens, B), None if starts is None else _ints("starts", starts, B),
                                _ptr(out), _ptr(lse), B, H, Hkv, N, C, R, page, n_pages, blocks, bool(causal), code, phi_code,
-                               bool(phi_batch_broadcast), scale, _ptr(workspace), ws_bytes, _stream(stream))
+                               bool(phi_batch_broadcast), float(scale), _ptr(workspace), ws_bytes, handle)
     _check(st, "fb_paged_attn_fwd")
     return out, lse

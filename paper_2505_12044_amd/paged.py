@@ -28,6 +28,8 @@ class PagedCache:
         cached beside the keys (0: none)."""
         if min(layers, requests, kv_heads, n_pages, max_tokens) < 1 or rank < 0:
             raise api.FlashBiasError("sizes must be positive")
+        if page not in (16, 32, 64, 128, 256):
+            raise api.FlashBiasError("page must be 16, 32, 64, 128 or 256")
         self.page = page
         shape = (layers, n_pages, kv_heads, page)
         self.k_pages = torch.empty((*shape, head_dim), dtype=dtype, device=device)

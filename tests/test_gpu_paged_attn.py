@@ -210,3 +210,51 @@ def test_side_stream_and_workspace_of_the_caller():
         s.synchronize()
         for x in (got, own):
             assert torch.equal(x[0], want[0]) and torch.equal(x[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_new_tokens(dtype):
+    run(2, 100, 6, 2, 64, 16, [100, 611], dtype, "alibi")
+    run(1, 130, 2, 2, 32, 32, [90], dtype, "factors", 2)            # more queries than keys: the first see nothing
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("length", [50, 3000])
+def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, length):
+    c = make_cache([length, length], 2, 16, 64, 0, dtype, F32, 6)
+    q = randn(torch.Generator().manual_seed(8), (2, 4, 1, 64), dtype)
+    clean = api.fb_paged_attn_fwd(q, c["k_pages"], c["v_pages"], c["table"], c["lens"])
+    bad = q.clone()
+    bad[0, 1, 0, 5] = math.nan                                        # one head's query
+    bad[0, 2, 0, 7] = math.inf                                        # scores of both infinities
+    o, l = api.fb_paged_attn_fwd(bad, c["k_pages"], c["v_pages"], c["table"], c["lens"])
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(4):
+            if b == 0 and h in (1, 2):
+                assert torch.isnan(o[b, h]).all() and torch.isnan(l[b, h]).all()
+            else:
+                assert torch.equal(o[b, h], clean[0][b, h]) and torch.equal(l[b, h], clean[1][b, h])
+    k = c["k_pages"].clone()
+    k[c["table"][1, 1].long(), 1, 3] = math.nan                       # one key of request 1's second key head
+    o, l = api.fb_paged_attn_fwd(q, k, c["v_pages"], c["table"], c["lens"])
+    torch.cuda.synchronize()
+    assert torch.isnan(o[1, 2:]).all() and torch.isnan(l[1, 2:]).all()
+    assert torch.equal(o[0], clean[0][0]) and torch.equal(o[1, :2], clean[0][1, :2])
+
+
+def test_calls_on_two_streams_at_once():
+    cs = [make_cache([4000, 300], 2, 16, 64, 0, BF, F32, s) for s in (3, 4)]
+    qs = [randn(torch.Generator().manual_seed(s), (2, 8, 1, 64), BF) for s in (5, 6)]
+    args = [(q, c["k_pages"], c["v_pages"], c["table"], c["lens"]) for q, c in zip(qs, cs)]
+    want = [api.fb_paged_attn_fwd(*a) for a in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in args]
+    got = []
+    for _ in range(10):
+        for s, a in zip(streams, args):
+            with torch.cuda.stream(s):
+                got.append(api.fb_paged_attn_fwd(*a))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert torch.equal(g[0], want[i % 2][0]) and torch.equal(g[1], want[i % 2][1])
