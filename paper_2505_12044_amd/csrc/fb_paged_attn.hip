@@ -31,8 +31,11 @@ namespace {
 constexpr int kPaWaves = 4;
 constexpr int kPaThreads = kPaWaves * 64;
 constexpr int kPaRows = 16;
-constexpr int kPaLeast = 2;       // steps of a worker's share at least (the join of smaller shares costs more than they save)
-constexpr int kPaLead = 2;        // steps that a group's beginning and end cost, counted into the shares
+// Costs of a worker's share at least, and the steps that a group's beginning and end count for in the shares.  us at 1, 2, 3 of
+// the first: B 4, H 8 / 4, fp32 drafts 21.2, 17.9, 17.2; B 8, H 16, 100 to 1024 keys 13.5, 13.5, 14.9; of the second: encoder
+// states (B 48, 1 to 1500 keys, 12 heads) 25.2, 25.0 and, not counted, 27.9; B 8, 100 to 1024 keys 13.7, 13.5, 15.1.
+constexpr int kPaLeast = 2;
+constexpr int kPaLead = 2;
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
@@ -66,7 +69,9 @@ FB_DEV float weight(float a, float m) { return a == -INFINITY ? 0.f : fast_exp2(
 template <typename T, int C, int GROUPS>
 struct Step;
 constexpr int step_groups(int c, bool f32) { return (c <= 32 ? 4 : 2) / (f32 ? 2 : 1); }
-constexpr int waves_per_simd(int c) { return c == 16 ? 4 : 2; }
+// Waves a SIMD has, and the launch counts on.  us at 2, 3, 4: B 48 encoder states to 8000, C 64 86, 82, 84; B 64, M 8192, C 16
+// 75, 62, 63; C 32 103, 107, 107; C 128 has no registers for three.
+constexpr int waves_per_simd(int c) { return c == 16 ? 4 : (c == 64 ? 3 : 2); }
 
 template <int C, int GROUPS>
 struct Step<bf16_t, C, GROUPS> {
@@ -798,7 +803,10 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 
 }  // namespace
 
-// Waves that share the keys: all that are resident, two per SIMD.  Requests of at most 512 keys are not split.
+// Waves that share the keys: all that are resident.  Requests of at most five turns of a workgroup's four waves are not split:
+// a turn takes a memory latency, 1.2 us, the split's bookkeeping and its join 5 us.  us without / with the split, 16 groups:
+// bf16 C 64 512 keys 7.7 / 10.3, 1024 keys 11.6 / 10.5; C 128 9.5 / 12.2, 14.2 / 12.8; fp32 C 64 300 keys 8.9 / 10.9, 512 keys
+// 11.6 / 10.9; 1024 groups, bf16 C 128, 512 keys 52 / 54, 1024 keys 99 / 99.
 int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32) {
     const int step = 16 * step_groups(C, f32);
     const long long steps = (capacity + step - 1) / step;
