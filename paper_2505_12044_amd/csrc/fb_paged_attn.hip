@@ -803,14 +803,16 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 
 }  // namespace
 
-// Waves that share the keys: all that are resident.  Requests of at most five turns of a workgroup's four waves are not split:
-// a turn takes a memory latency, 1.2 us, the split's bookkeeping and its join 5 us.  us without / with the split, 16 groups:
-// bf16 C 64 512 keys 7.7 / 10.3, 1024 keys 11.6 / 10.5; C 128 9.5 / 12.2, 14.2 / 12.8; fp32 C 64 300 keys 8.9 / 10.9, 512 keys
-// 11.6 / 10.9; 1024 groups, bf16 C 128, 512 keys 52 / 54, 1024 keys 99 / 99.
+// Waves that share the keys: all that are resident.  Short requests (by the table's width) are not split: a turn of a workgroup's
+// four waves takes a memory latency, 1.2 us at C = 64 and 1.7 at 128, the split's bookkeeping, its join and the launch of
+// that 5 us on either side of the queue.  us without / with the split, on the GPU; as calls one after the other:
+//   bf16 C 64, 16 groups 1024 keys 10.6 / 11.0; 11.6 / 16.5, 1536 keys 16.5 / 11.2; 15.7 / 16.2; 1024 groups 1024 keys 46 / 50; 44 / 50
+//   bf16 C 128, 16 groups 640 keys 11.6 / 13.0; 11.4 / 16.2, 1024 keys 16.8 / 13.2; 16.2 / 16.2
+//   fp32 C 64, 16 groups 512 keys 11.2 / 11.2; 11.7 / 16.3, 768 keys 16.0 / 11.4; 15.4 / 16.5; C 128 320 keys 12.6 / 14.3; 11.7 / 16.1
 int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32) {
     const int step = 16 * step_groups(C, f32);
     const long long steps = (capacity + step - 1) / step;
-    if (capacity <= (f32 ? 320 : 640)) return 0;
+    if (capacity <= (C == 128 ? 640 : 1024) / (f32 ? 2 : 1)) return 0;
     int cus = fb_cu_count();
     if (cus <= 0) cus = 256;
     const long long groups = (long long)B * Hkv * row_tiles;

@@ -14,8 +14,8 @@ BF, F32 = torch.bfloat16, torch.float32
 
 
 def run(B, N, H, Hkv, C, page, lens, dtype=BF, bias="none", R=0, phi=F32, causal=True, shared=False, starts=None, seed=1,
-        scale=0.0, workspace="own"):
-    c = make_cache(lens, Hkv, page, C, R, dtype, phi, seed)
+        scale=0.0, workspace="own", room=1):
+    c = make_cache(lens, Hkv, page, C, R, dtype, phi, seed, extra_blocks=room)
     g = torch.Generator().manual_seed(seed + 1)
     q = randn(g, (B, H, N, C), dtype)
     phi_q = randn(g, (1 if shared else B, H, N, R), phi, R ** -0.25) if R else None
@@ -258,3 +258,23 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for i, g in enumerate(got):
         assert torch.equal(g[0], want[i % 2][0]) and torch.equal(g[1], want[i % 2][1])
+
+
+@pytest.mark.parametrize("C", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("bias,R", [("none", 0), ("alibi", 0), ("factors", 2), ("factors", 8), ("factors", 9)])
+def test_short_requests_in_a_wide_table(C, dtype, bias, R):
+    # room for long requests: the keys are split over the GPU whatever the lengths are
+    run(6, 2, 6, 2, C, 16, [0, 1, 33, 64, 130, 515], dtype, bias, R, starts=[0, 0, 31, 62, 129, 513], room=300)
+
+
+@pytest.mark.parametrize("length", [1, 2, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 257, 1000])
+def test_lengths_in_a_wide_table(length):
+    run(1, 1, 2, 1, 64, 16, [length], BF, "alibi", room=400, seed=length)
+    run(1, 1, 2, 1, 64, 256, [length], F32, "none", room=30, seed=length)
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 256, 257, 700])
+def test_numbers_of_requests(B):
+    rng = np.random.default_rng(B)
+    run(B, 1, 2, 1, 32, 16, rng.integers(0, 200, B), BF, "alibi", room=200, seed=B)
