@@ -17,7 +17,7 @@
 // waves takes an equal share, found from the lengths on the device: one long request among short ones, or a table with
 // room for far more than it holds, costs no balance, and no wave waits for another.  A share may end inside a group: the
 // parts go to scratch, two per worker at most, and a second launch joins them in a fixed order.  Without scratch, and
-// where no request can be long, a workgroup's four waves share one group and join through LDS.
+// where no request can be long, a workgroup's waves share one group and join through LDS.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -30,6 +30,8 @@ namespace {
 
 constexpr int kPaWaves = 4;
 constexpr int kPaThreads = kPaWaves * 64;
+constexpr size_t group_lds(int waves, int rows, int c) { return (size_t)waves * rows * (c + 6) * sizeof(float); }
+constexpr int pa_threads(int w) { return w == 1 ? kPaThreads : w * 64; }
 constexpr int kPaRows = 16;
 // Costs of a worker's share at least, and the steps that a group's beginning and end count for in the shares.  us at 1, 2, 3 of
 // the first: B 4, H 8 / 4, fp32 drafts 21.2, 17.9, 17.2; B 8, H 16, 100 to 1024 keys 13.5, 13.5, 14.9; of the second: encoder
@@ -69,7 +71,7 @@ FB_DEV float weight(float a, float m) { return a == -INFINITY ? 0.f : fast_exp2(
 template <typename T, int C, int GROUPS>
 struct Step;
 constexpr int step_groups(int c, bool f32) { return (c <= 32 ? 4 : 2) / (f32 ? 2 : 1); }
-// Waves a SIMD has, and the launch counts on.  us at 2, 3, 4: B 48 encoder states to 8000, C 64 86, 82, 84; B 64, M 8192, C 16
+// Waves a SIMD has where each has its own share, and the launch counts on.  us at 2, 3, 4: B 48 encoder states to 8000, C 64 86, 82, 84; B 64, M 8192, C 16
 // 75, 62, 63; C 32 103, 107, 107; C 128 has no registers for three.
 constexpr int waves_per_simd(int c) { return c == 16 ? 4 : (c == 64 ? 3 : 2); }
 
@@ -309,12 +311,14 @@ struct Segment {
 };
 
 // BIAS, PF32: kind of bias and whether the factors are float
-template <typename T, int C, int BIAS, bool PF32, bool SPLIT>
-__global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kernel(PagedAttnParams p) {
+// W: waves that share a group, one workgroup (4 or 8), or 1: each wave has its own share of all groups
+template <typename T, int C, int BIAS, bool PF32, int W>
+__global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void paged_attn_kernel(PagedAttnParams p) {
+    constexpr bool SPLIT = W == 1;
     constexpr int GROUPS = step_groups(C, std::is_same_v<T, float>);
     using S = Step<T, C, GROUPS>;
     constexpr int KW = S::KW, NV = S::NV;
-    constexpr int STRIDE = SPLIT ? KW : kPaWaves * KW;    // keys from one step of a wave to its next
+    constexpr int STRIDE = W * KW;                        // keys from one step of a wave to its next
     constexpr int NF = BIAS == kBiasFactors4 ? 1 : (BIAS >= kBiasFactors16 ? 4 : 0);
     using PT = std::conditional_t<PF32, float, bf16_t>;
 
@@ -646,31 +650,34 @@ __global__ __launch_bounds__(kPaThreads, waves_per_simd(C)) void paged_attn_kern
                 }
             } else {
                 // ---- the waves of the workgroup ----
-                __shared__ __align__(16) float sm_o[kPaWaves][kPaRows][C + 4];      // + 4: rows start in different banks
-                __shared__ float sm_m[kPaWaves][kPaRows], sm_l[kPaWaves][kPaRows];
+                extern __shared__ __align__(16) float sm_parts[];
+                constexpr int PITCH = C + 4;                              // rows start in different banks
+                const int part_rows = min(kPaRows, rows_all);
+                float* sm_m = sm_parts + W * part_rows * PITCH;
+                float* sm_l = sm_m + W * part_rows;
                 if (has_row) {
 #pragma unroll
                     for (int r = 0; r < 4; r++)
 #pragma unroll
-                        for (int t = 0; t < NV; t++) sm_o[wave][i][(4 * g + r) * NV + t] = o[t][r];
+                        for (int t = 0; t < NV; t++) sm_parts[(wave * part_rows + i) * PITCH + (4 * g + r) * NV + t] = o[t][r];
                     if (g == 0) {
-                        sm_m[wave][i] = m;
-                        sm_l[wave][i] = l;
+                        sm_m[wave * part_rows + i] = m;
+                        sm_l[wave * part_rows + i] = l;
                     }
                 }
                 __syncthreads();
-                for (int x = tid; x < rows * (C / 4); x += kPaThreads) {
+                for (int x = tid; x < rows * (C / 4); x += pa_threads(W)) {
                     const int r = x / (C / 4), c4 = x % (C / 4);
-                    float mx = sm_m[0][r];
+                    float mx = sm_m[r];
 #pragma unroll
-                    for (int w = 1; w < kPaWaves; w++) mx = fmaxf(mx, sm_m[w][r]);
+                    for (int w = 1; w < W; w++) mx = fmaxf(mx, sm_m[w * part_rows + r]);
                     float lt = 0.f;
                     f32x4 ot = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int w = 0; w < kPaWaves; w++) {
-                        const float a = weight(sm_m[w][r], mx);
-                        const f32x4 y = *(const f32x4*)&sm_o[w][r][c4 * 4];
-                        lt = fmaf(a, sm_l[w][r], lt);
+                    for (int w = 0; w < W; w++) {
+                        const float a = weight(sm_m[w * part_rows + r], mx);
+                        const f32x4 y = *(const f32x4*)&sm_parts[(w * part_rows + r) * PITCH + c4 * 4];
+                        lt = fmaf(a, sm_l[w * part_rows + r], lt);
 #pragma unroll
                         for (int e = 0; e < 4; e++) ot[e] = fmaf(a, y[e], ot[e]);
                     }
@@ -752,15 +759,23 @@ __global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, in
     write_row<T, C>(p, (long long)b * p.H * p.N + (long long)h * (p.G * p.N) + r0 + r, c4, ot, lt, mx);
 }
 
+template <typename T, int C, int BIAS, bool PF32, int W>
+int launch_groups(const PagedAttnParams& p, hipStream_t stream) {
+    const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;
+    if (blocks >= (1LL << 31)) return -1;
+    const int rows = p.G * p.N < kPaRows ? p.G * p.N : kPaRows;
+    static FbLdsOnce once;
+    if (!fb_raise_lds_limit((const void*)paged_attn_kernel<T, C, BIAS, PF32, W>, group_lds(W, kPaRows, C), once)) return 1;
+    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, W>), dim3((unsigned)blocks), dim3(pa_threads(W)), group_lds(W, rows, C), stream, p);
+    return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+
 template <typename T, int C, int BIAS, bool PF32>
 int launch_attn(const PagedAttnParams& p, hipStream_t stream) {
     if (p.workers == 0) {
-        const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;
-        if (blocks >= (1LL << 31)) return -1;
-        hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, false>), dim3((unsigned)blocks), dim3(kPaThreads), 0, stream, p);
-        return hipGetLastError() == hipSuccess ? 0 : 1;
+        return p.waves == 8 ? launch_groups<T, C, BIAS, PF32, 8>(p, stream) : launch_groups<T, C, BIAS, PF32, 4>(p, stream);
     }
-    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, true>), dim3((unsigned)((p.workers + kPaWaves - 1) / kPaWaves)), dim3(kPaThreads), 0,
+    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, 1>), dim3((unsigned)((p.workers + kPaWaves - 1) / kPaWaves)), dim3(kPaThreads), 0,
                        stream, p);
     if (hipGetLastError() != hipSuccess) return 1;
     const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
@@ -804,7 +819,7 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 }  // namespace
 
 // Waves that share the keys: all that are resident.  Short requests (by the table's width) are not split: a turn of a workgroup's
-// four waves takes a memory latency, 1.2 us at C = 64 and 1.7 at 128, the split's bookkeeping, its join and the launch of
+// waves takes a memory latency, 1.2 us at C = 64 and 1.7 at 128, the split's bookkeeping, its join and the launch of
 // that 5 us on either side of the queue.  us without / with the split, on the GPU; as calls one after the other:
 //   bf16 C 64, 16 groups 1024 keys 10.6 / 11.0; 11.6 / 16.5, 1536 keys 16.5 / 11.2; 15.7 / 16.2; 1024 groups 1024 keys 46 / 50; 44 / 50
 //   bf16 C 128, 16 groups 640 keys 11.6 / 13.0; 11.4 / 16.2, 1024 keys 16.8 / 13.2; 16.2 / 16.2
@@ -842,5 +857,9 @@ int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream
         p.part_m = p.part_o + parts * C;
         p.part_l = p.part_m + parts;
     }
+    // Eight waves a group where every group has a CU of its own and four would take more than two turns.  us with four / eight,
+    // C 64: 16 groups 128 keys 4.5 / 5.3, 512 keys 7.3 / 6.6, 1024 keys 10.9 / 9.2; 128 groups 512 keys 8.9 / 7.3, 1024 keys 15.1 /
+    // 11.4; 576 groups 17.0 / 19.6, 28.5 / 31.5.  C 128, 128 groups, 512 keys 11.8 / 11.5; fp32 C 64 15.9 / 12.8.
+    p.waves = (long long)p.B * p.Hkv * p.row_tiles <= fb_cu_count() && capacity > 2 * 4 * 16 * step_groups(C, f32) ? 8 : 4;
     return f32 ? attn_channels<float>(p, C, stream) : attn_channels<bf16_t>(p, C, stream);
 }

@@ -126,6 +126,7 @@ struct PagedAttnParams {
     int G, capacity;         // set by the launch: H / Hkv; keys that a table row has room for
     float inv_n;             // 1 / N
     int workers;             // waves the keys are split over; 0: a workgroup per key head and row tile, no split
+    int waves;               // of such a workgroup, set by the launch
     int joins_by_group;      // joins has an entry per (request, key head, row tile), else one per worker
     float* part_o;           // scratch: two parts per worker, [workers, 2, rows, C], rows = min(16, H / Hkv * N)
     float* part_m;           // [workers, 2, rows] maxima
