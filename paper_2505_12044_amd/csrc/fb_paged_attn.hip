@@ -65,14 +65,15 @@ FB_DEV float weight(float a, float m) { return a == -INFINITY ? 0.f : fast_exp2(
 // ---- one step of a wave: KW keys against 16 rows -----------------------------------------------
 // Values are read past the caches (each row once, by whole lines): B 32 H 32 / 8 C 128 152 -> 139 us, C 64 128 -> 108 us at
 // 604 MB.  Keys are not: half a line per load instruction, and the same figures within 3 % either way.
-// KW: as many as 64 registers of keys and values hold, up to 64 (a wave has one step in flight, and a step takes a
-// memory latency at least: 32 keys a step at 64 channels are slower).
+// KW: 32 keys in bf16, 16 in fp32, twice that below 64 channels, where a row is little.  A wave has one step in flight and a
+// step takes a memory latency, but fewer keys a step reach more waves: C 64, 576 groups of 500 keys, 32 / 64 keys a step 16.8 /
+// 19.3 us, C 128 drafts and long batches 5 % apart; C 32, 1024 groups of 8192 keys 222 / 186 us.
 // Lane l: g = l / 16, i = l % 16.  S^T group s (16 keys): column i (the query row), keys 4 g + r.
 template <typename T, int C, int GROUPS>
 struct Step;
 constexpr int step_groups(int c, bool f32) { return (c <= 32 ? 4 : 2) / (f32 ? 2 : 1); }
-// Waves a SIMD has where each has its own share, and the launch counts on.  us at 2, 3, 4: B 48 encoder states to 8000, C 64 86, 82, 84; B 64, M 8192, C 16
-// 75, 62, 63; C 32 103, 107, 107; C 128 has no registers for three.
+// Waves a SIMD has where each has its own share, and the launch counts on.  us at 2, 3, 4: B 48 encoder states to 8000 keys, C 64
+// 86, 82, 84; B 64 to 8192 keys, C 16 75, 62, 63, C 32 103, 107, 107; C 128 has no registers for three.
 constexpr int waves_per_simd(int c) { return c == 16 ? 4 : (c == 64 ? 3 : 2); }
 
 template <int C, int GROUPS>
@@ -764,8 +765,10 @@ int launch_groups(const PagedAttnParams& p, hipStream_t stream) {
     const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;
     if (blocks >= (1LL << 31)) return -1;
     const int rows = p.G * p.N < kPaRows ? p.G * p.N : kPaRows;
-    static FbLdsOnce once;
-    if (!fb_raise_lds_limit((const void*)paged_attn_kernel<T, C, BIAS, PF32, W>, group_lds(W, kPaRows, C), once)) return 1;
+    if constexpr (group_lds(W, kPaRows, C) > 65536) {
+        static FbLdsOnce once;
+        if (!fb_raise_lds_limit((const void*)paged_attn_kernel<T, C, BIAS, PF32, W>, group_lds(W, kPaRows, C), once)) return 1;
+    }
     hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, W>), dim3((unsigned)blocks), dim3(pa_threads(W)), group_lds(W, rows, C), stream, p);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
