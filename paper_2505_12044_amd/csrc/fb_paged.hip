@@ -13,11 +13,12 @@ namespace {
 // b gets its pages if the needs of 0..b add up to no more than there are.  Token i of the call is o + i.
 //
 // Bound by latency: a few reads per request and one written int or two per token.  One launch: every workgroup sums
-// the whole batch's needs by itself (two scans of at most 4096 lengths from L2), so nothing is handed over between
-// workgroups, and then owns kPlanItems tokens of [B, N].  us for B 64 N 1; B 256 N 4096; B 1024 N 1; B 4096 N 1: with 512
-// threads and tokens 6.2, 9.8, 9.9, 14.0; 256 each 6.0, 9.6, 10.4, 17.7; 1024 each 6.8, 13.8, 11.2, 13.9.  The thread of a page's first token enters the page in the
+// the whole batch's needs by itself (a scan of at most 4096 lengths from L2), so nothing is handed over between
+// workgroups, and then owns kPlanItems tokens of [B, N].  The thread of a page's first token enters the page in the
 // table.  A page taken in the same call in which it was given back is looked up where it comes from (a shrinking
 // request's table row, which no one writes), not in the ring, which another workgroup may not have written yet.
+// us for B 64 N 1; B 256 N 4096; B 1024 N 1; B 4096 N 1: with 512 threads and tokens 6.2, 9.8, 9.9, 14.0; 256 each 6.0, 9.6,
+// 10.4, 17.7; 1024 each 6.8, 13.8, 11.2, 13.9.
 constexpr int kPlanThreads = 512;
 constexpr int kPlanItems = 512;
 

@@ -102,9 +102,11 @@ struct Step<bf16_t, C, GROUPS> {
 #pragma unroll
         for (int u = 0; u < NU; u++) {
             if constexpr (C == 16)
-                acc = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, k.x[s][u]), __builtin_bit_cast(s16x4, q.x[u]), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, k.x[s][u]), __builtin_bit_cast(s16x4, q.x[u]), acc,
+                                                                0, 0, 0);
             else
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k.x[s][u]), __builtin_bit_cast(bf16x8, q.x[u]), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k.x[s][u]), __builtin_bit_cast(bf16x8, q.x[u]), acc,
+                                                              0, 0, 0);
         }
         return acc;
     }
@@ -786,8 +788,8 @@ int launch_attn(const PagedAttnParams& p, hipStream_t stream) {
     // slots: as many parts at a time as a group has on average, the rest are rows
     const long long parts = p.workers / groups;
     const int lanes = parts >= 6 ? 8 : (parts >= 3 ? 4 : 2);
-    hipLaunchKernelGGL((paged_join_kernel<T, C>), dim3((unsigned)(p.joins_by_group ? groups : p.workers), (unsigned)((rows * lanes + 7) / 8)), dim3(2 * C),
-                       0, stream, p, lanes);
+    const dim3 grid((unsigned)(p.joins_by_group ? groups : p.workers), (unsigned)((rows * lanes + 7) / 8));
+    hipLaunchKernelGGL((paged_join_kernel<T, C>), grid, dim3(2 * C), 0, stream, p, lanes);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

@@ -136,7 +136,8 @@ int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream) {
     const int size = f32 ? 4 : 2;
     long long bits = p.pairs | (16 / size);
     const auto starts = [&](const RotaryTensor& t, int heads) {          // strides of axes of one element do not count
-        if (heads > 0) bits |= (long long)(reinterpret_cast<uintptr_t>(t.x) / size) | (p.B > 1 ? t.sb : 0) | (heads > 1 ? t.sh : 0) | (p.N > 1 ? t.sn : 0);
+        if (heads > 0)
+            bits |= (long long)(reinterpret_cast<uintptr_t>(t.x) / size) | (p.B > 1 ? t.sb : 0) | (heads > 1 ? t.sh : 0) | (p.N > 1 ? t.sn : 0);
     };
     starts(p.t0, p.H0);
     starts(p.t1, p.H1);
