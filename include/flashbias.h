@@ -387,7 +387,7 @@ int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* 
  *   encoder).  Keys in a table entry that is no page are not seen; lens are cut to [0, max_blocks * page].  What lies in the pages behind the
  *   last token, or in rows a query does not see, never reaches the result.  A query that sees nothing, or scores of -infinity
  *   only, has out = 0 and lse = -infinity.
- *   N is meant to be small: every 16 of a key head's H / Hkv * N query rows read its keys again (H / Hkv * N < 2^24).
+ *   N is meant to be small: every 16 or 32 of a key head's H / Hkv * N query rows read its keys again (H / Hkv * N < 2^24).
  *   dtype FB_BF16 (products in bf16, probabilities in two bf16 limbs, everything else fp32) or FB_F32 (all fp32, fp32 factors).
  *   workspace: device scratch of fb_paged_attn_fwd_workspace_bytes(...) bytes, 16-byte aligned, contents ignored, for the parts
  *   of key heads that several workgroups share; without it (NULL, or too small) a key head stays in one workgroup.

@@ -727,18 +727,8 @@ int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* 
     return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
 }
 
-// Row tiles of a key head, the waves a call is split over, and the scratch for them.
-struct PagedSplit {
-    int row_tiles, workers;
-    size_t bytes;
-};
-static PagedSplit paged_split(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {
-    const long long rows = (long long)(H / Hkv) * N;
-    PagedSplit s;
-    s.row_tiles = (int)((rows + 15) / 16);
-    s.workers = fb_paged_attn_workers(B, Hkv, s.row_tiles, (long long)max_blocks * page, C, dtype == FB_F32);
-    s.bytes = s.workers ? fb_paged_attn_workspace_bytes(s.workers, (long long)B * Hkv * s.row_tiles, rows, C) : 0;
-    return s;
+static PagedAttnSplit paged_split(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {
+    return fb_paged_attn_split(B, Hkv, (long long)(H / Hkv) * N, (long long)max_blocks * page, C, dtype == FB_F32);
 }
 
 size_t fb_paged_attn_fwd_workspace_bytes(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {
@@ -775,8 +765,8 @@ int fb_paged_attn_fwd(const void* q, const void* k_pages, const void* v_pages,
     p.B = B; p.H = H; p.Hkv = Hkv; p.N = N; p.R = R; p.page_shift = page_shift_of(page); p.n_pages = n_pages;
     p.max_blocks = max_blocks; p.causal = causal != 0; p.phi_f32 = phi_dtype == FB_F32;
     p.scale = scale > 0.f ? scale : 1.0f / std::sqrt((float)C);
-    const PagedSplit split = paged_split(B, H, Hkv, N, C, page, max_blocks, dtype);
-    p.row_tiles = split.row_tiles;
+    const PagedAttnSplit split = paged_split(B, H, Hkv, N, C, page, max_blocks, dtype);
+    p.tile_rows = split.tile_rows; p.row_tiles = split.row_tiles;
     // without room for the parts a key head stays in one workgroup
     p.workers = workspace && workspace_bytes >= split.bytes ? split.workers : 0;
     const int rc = fb_launch_paged_attn(p, C, dtype == FB_F32, workspace, (hipStream_t)stream);

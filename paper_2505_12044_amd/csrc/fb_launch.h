@@ -64,10 +64,13 @@ int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream);
 constexpr int kFbPlanRequests = 4096;       // requests one plan takes
 int fb_launch_paged_plan(const PagedPlanParams& p, hipStream_t stream);
 int fb_launch_paged_append(PagedAppendParams p, bool f32, bool phi_f32, hipStream_t stream);
-// Waves that share the keys of a call whose requests have up to `capacity` keys each, 0: no split (no scratch).
-int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32);
-// groups: B * Hkv * row_tiles; rows: query rows of a key head
-size_t fb_paged_attn_workspace_bytes(int workers, long long groups, long long rows, int C);
+// How a call whose requests have up to `capacity` keys is split: the rows (query rows of a key head) into row_tiles tiles of
+// tile_rows, the keys over so many waves (workers, 0: no split) with so many bytes of scratch.
+struct PagedAttnSplit {
+    int tile_rows, row_tiles, workers;
+    size_t bytes;
+};
+PagedAttnSplit fb_paged_attn_split(int B, int Hkv, long long rows, long long capacity, int C, bool f32);
 int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream_t stream);
 
 // A kernel's dynamic-LDS limit is an attribute of the (kernel, device) pair: raise it on the

@@ -5,7 +5,8 @@
 // heads share a key head, so the G N rows that meet the same keys form one tile of 16 rows (several where there are more).
 //
 // Bound by memory: every key and value row is read once per row tile, 4 C flops per row and key against 4 C bytes per
-// key (bf16).  The matrix pipe has twenty times the rate that needs, so the 16-row tile runs whatever G N is:
+// key (bf16).  The matrix pipe has twenty times the rate that needs, so the 16-row tile runs whatever G N is (and where there
+// are more rows a wave takes two tiles at once, RT: B 32, H 32 / 8, N 5, 500 to 16384 keys 239 -> 153 us, N 16 454 -> 272):
 //   scores   S^T = K Q^T      keys are the rows of the A operand, read from their page straight into its layout
 //   values   O^T += V^T P^T   P^T comes from the S^T registers as they are; a lane loads NV = C / 16 adjacent channels of
 //                             its eight keys (whole rows per 16 lanes) and turns 8 x NV into operands by byte permutes
@@ -32,7 +33,6 @@ constexpr int kPaWaves = 4;
 constexpr int kPaThreads = kPaWaves * 64;
 constexpr size_t group_lds(int waves, int rows, int c) { return (size_t)waves * rows * (c + 6) * sizeof(float); }
 constexpr int pa_threads(int w) { return w == 1 ? kPaThreads : w * 64; }
-constexpr int kPaRows = 16;
 // Costs of a worker's share at least, and the steps that a group's beginning and end count for in the shares.  us at 1, 2, 3 of
 // the first: B 4, H 8 / 4, fp32 drafts 21.2, 17.9, 17.2; B 8, H 16, 100 to 1024 keys 13.5, 13.5, 14.9; of the second: encoder
 // states (B 48, 1 to 1500 keys, 12 heads) 25.2, 25.0 and, not counted, 27.9; B 8, 100 to 1024 keys 13.7, 13.5, 15.1.
@@ -74,7 +74,8 @@ struct Step;
 constexpr int step_groups(int c, bool f32) { return (c <= 32 ? 4 : 2) / (f32 ? 2 : 1); }
 // Waves a SIMD has where each has its own share, and the launch counts on.  us at 2, 3, 4: B 48 encoder states to 8000 keys, C 64
 // 86, 82, 84; B 64 to 8192 keys, C 16 75, 62, 63, C 32 103, 107, 107; C 128 has no registers for three.
-constexpr int waves_per_simd(int c) { return c == 16 ? 4 : (c == 64 ? 3 : 2); }
+constexpr int waves_per_simd(int c, int tiles) { return tiles > 1 ? 2 : (c == 16 ? 4 : (c == 64 ? 3 : 2)); }
+constexpr bool two_tiles(int c, bool f32) { return c >= 64 && !f32; }    // whether a step may serve 32 rows
 
 template <int C, int GROUPS>
 struct Step<bf16_t, C, GROUPS> {
@@ -315,9 +316,11 @@ struct Segment {
 
 // BIAS, PF32: kind of bias and whether the factors are float
 // W: waves that share a group, one workgroup (4 or 8), or 1: each wave has its own share of all groups
-template <typename T, int C, int BIAS, bool PF32, int W>
-__global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void paged_attn_kernel(PagedAttnParams p) {
+// RT: tiles of 16 query rows that a step serves
+template <typename T, int C, int BIAS, bool PF32, int W, int RT>
+__global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C, RT) : 2) void paged_attn_kernel(PagedAttnParams p) {
     constexpr bool SPLIT = W == 1;
+    constexpr int ROWS = 16 * RT;
     constexpr int GROUPS = step_groups(C, std::is_same_v<T, float>);
     using S = Step<T, C, GROUPS>;
     constexpr int KW = S::KW, NV = S::NV;
@@ -420,49 +423,58 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void
     pages_at(f_page, f, fk);
     bool have = false, more = true;                       // a step is loaded; one is to be loaded
 
-    // of the segment: the lane's query row, its sums
-    bool has_row = false;
-    int pos = 0, limit = 0, all_see = 0, rows = 0, h = 0;
+    // of the segment: the lane's query row in each tile, its sums
+    struct Row {
+        bool has;
+        int pos, limit;                                   // limit: keys the row sees
+        typename S::Query q;
+        float phi_q[NF > 0 ? NF : 1], slope, m, l;
+        const PT* pq;
+        f32x4 o[NV];
+    } row[RT];
+    int all_see = 0, rows = 0, h = 0;
     long long row_base = 0;
-    typename S::Query q = {};
-    float phi_q[NF > 0 ? NF : 1] = {}, slope = 0.f, m = -INFINITY, l = 0.f;
-    const PT* pq_row = nullptr;
-    f32x4 o[NV];
 
     // ---- a segment (s) begins ----
     auto begin = [&]() __attribute__((always_inline)) {
         h = p.row_tiles == 1 ? s.grp : s.grp / p.row_tiles;
-        const int r0 = (s.grp - h * p.row_tiles) * kPaRows;
-        rows = min(kPaRows, rows_all - r0);
+        const int r0 = (s.grp - h * p.row_tiles) * ROWS;
+        rows = min(ROWS, rows_all - r0);
         row_base = (long long)s.b * p.H * p.N + (long long)h * rows_all + r0;       // of q, out, lse
-        has_row = i < rows;
-        // (r0 + i) / N and the rest, rows below 2^24
-        int head = (int)((float)(r0 + i) * p.inv_n);
-        int n = r0 + i - head * p.N;
-        if (n < 0) head--, n += p.N;
-        else if (n >= p.N) head++, n -= p.N;
-        pos = s.start + n;
-        limit = !has_row ? 0 : (p.causal ? (pos >= s.len || pos < 0 ? 0 : pos + 1) : s.len);     // keys the row sees
-        all_see = p.causal ? max(min(s.start + 1, s.len), 0) : s.len;                           // keys every row sees
+        all_see = p.causal ? max(min(s.start + 1, s.len), 0) : s.len;                // keys every row sees
 #pragma unroll
-        for (int x = 0; x < S::NU; x++) {
-            q.x[x] = {};
-            if (has_row) q.x[x] = S::row_chunk((const T*)p.q + (row_base + i) * C, g, x);
-        }
-        if constexpr (NF > 0) {
-            pq_row = (const PT*)p.phi_q + (long long)s.b * p.phiq_bstride + ((long long)h * rows_all + r0 + i) * p.R;
+        for (int rt = 0; rt < RT; rt++) {
+            Row& w = row[rt];
+            const int at = 16 * rt + i;
+            w.has = at < rows;
+            // (r0 + at) / N and the rest, rows below 2^24
+            int head = (int)((float)(r0 + at) * p.inv_n);
+            int n = r0 + at - head * p.N;
+            if (n < 0) head--, n += p.N;
+            else if (n >= p.N) head++, n -= p.N;
+            w.pos = s.start + n;
+            w.limit = !w.has ? 0 : (p.causal ? (w.pos >= s.len || w.pos < 0 ? 0 : w.pos + 1) : s.len);
 #pragma unroll
-            for (int x = 0; x < NF; x++) {
-                phi_q[x] = 0.f;
-                if (has_row && NF * g + x < p.R) phi_q[x] = (float)pq_row[NF * g + x];
+            for (int x = 0; x < S::NU; x++) {
+                w.q.x[x] = {};
+                if (w.has) w.q.x[x] = S::row_chunk((const T*)p.q + (row_base + at) * C, g, x);
             }
-        }
-        if constexpr (BIAS == kBiasAlibi)
-            if (has_row) slope = p.slopes[h * p.G + head];
-        m = -INFINITY;
-        l = 0.f;
+            if constexpr (NF > 0) {
+                w.pq = (const PT*)p.phi_q + (long long)s.b * p.phiq_bstride + ((long long)h * rows_all + r0 + at) * p.R;
 #pragma unroll
-        for (int t = 0; t < NV; t++) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < NF; x++) {
+                    w.phi_q[x] = 0.f;
+                    if (w.has && NF * g + x < p.R) w.phi_q[x] = (float)w.pq[NF * g + x];
+                }
+            }
+            w.slope = 0.f;
+            if constexpr (BIAS == kBiasAlibi)
+                if (w.has) w.slope = p.slopes[h * p.G + head];
+            w.m = -INFINITY;
+            w.l = 0.f;
+#pragma unroll
+            for (int t = 0; t < NV; t++) w.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     };
     auto load_keys = [&]() __attribute__((always_inline)) {              // of step f, fk
         const int fh = p.row_tiles == 1 ? f.grp : f.grp / p.row_tiles;
@@ -509,7 +521,7 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void
     }
 
     for (;;) {
-        f32x4 sc[GROUPS];
+        f32x4 sc[RT][GROUPS];
         int held = 0;
         bool whole = false;
         if (have) {
@@ -520,78 +532,104 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void
             whole = k0 + KW <= all_see && held == (1 << GROUPS) - 1;
 #pragma unroll
             for (int x = 0; x < GROUPS; x++) {
-                sc[x] = S::scores(kr, x, q);
                 const int key0 = k0 + 16 * x + 4 * g;
+                f32x4 bias[RT];
                 if constexpr (NF > 0) {
-                    f32x4 b = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int y = 0; y < NF; y++) b = __builtin_amdgcn_mfma_f32_16x16x4f32(factor(fr[x], y), phi_q[y], b, 0, 0, 0);
+                    for (int rt = 0; rt < RT; rt++) {
+                        bias[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int y = 0; y < NF; y++)
+                            bias[rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(factor(fr[x], y), row[rt].phi_q[y], bias[rt], 0, 0, 0);
+                    }
                     if constexpr (BIAS == kBiasFactors) {
                         const PT* pk = (const PT*)p.phi_pages + (row_at(page[x], h, k0 + 16 * x) + i) * p.R;
                         for (int y = 4; 4 * y < p.R; y++) {
                             const bool in = 4 * y + g < p.R;
-                            const float a = in ? (float)pk[4 * y + g] : 0.f, c = in && has_row ? (float)pq_row[4 * y + g] : 0.f;
-                            b = __builtin_amdgcn_mfma_f32_16x16x4f32(a, c, b, 0, 0, 0);
+                            const float a = in ? (float)pk[4 * y + g] : 0.f;
+#pragma unroll
+                            for (int rt = 0; rt < RT; rt++) {
+                                const float f = in && row[rt].has ? (float)row[rt].pq[4 * y + g] : 0.f;
+                                bias[rt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, f, bias[rt], 0, 0, 0);
+                            }
                         }
                     }
+                }
 #pragma unroll
-                    for (int r = 0; r < 4; r++) sc[x][r] = fmaf(sc[x][r], p.scale, b[r]);
-                } else {
+                for (int rt = 0; rt < RT; rt++) {
+                    f32x4 z = S::scores(kr, x, row[rt].q);
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        sc[x][r] *= p.scale;
-                        if constexpr (BIAS == kBiasAlibi) sc[x][r] = fmaf(slope, (float)(key0 + r - pos), sc[x][r]);
+                        if constexpr (NF > 0) z[r] = fmaf(z[r], p.scale, bias[rt][r]);
+                        else z[r] *= p.scale;
+                        if constexpr (BIAS == kBiasAlibi) z[r] = fmaf(row[rt].slope, (float)(key0 + r - row[rt].pos), z[r]);
                     }
-                }
-                if (!whole) {
+                    if (!whole) {
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
-                        if (key0 + r >= limit || !(held >> x & 1)) sc[x][r] = -INFINITY;
+                        for (int r = 0; r < 4; r++)
+                            if (key0 + r >= row[rt].limit || !(held >> x & 1)) z[r] = -INFINITY;
+                    }
+                    sc[rt][x] = z;
                 }
             }
         }
         if (more) load_keys();
         if (have) {
             // ---- softmax of the rows ----
-            float mx = m;
+            typename S::Probs pr[RT];
 #pragma unroll
-            for (int x = 0; x < GROUPS; x++)
+            for (int rt = 0; rt < RT; rt++) {
+                Row& w = row[rt];
+                float mx = w.m;
 #pragma unroll
-                for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[x][r]);
-            mx = column_max(mx);
-            if (__any(mx > m)) {
-                const float alpha = weight(m, mx);
-                l *= alpha;
+                for (int x = 0; x < GROUPS; x++)
 #pragma unroll
-                for (int t = 0; t < NV; t++)
+                    for (int r = 0; r < 4; r++) mx = fmaxf(mx, sc[rt][x][r]);
+                mx = column_max(mx);
+                if (__any(mx > w.m)) {
+                    const float alpha = weight(w.m, mx);
+                    w.l *= alpha;
 #pragma unroll
-                    for (int r = 0; r < 4; r++) o[t][r] *= alpha;
-                m = mx;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
+                    for (int t = 0; t < NV; t++)
 #pragma unroll
-            for (int x = 0; x < GROUPS; x++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    sc[x][r] = fast_exp2((sc[x][r] - ref) * kLog2e);
-                    l += sc[x][r];
+                        for (int r = 0; r < 4; r++) w.o[t][r] *= alpha;
+                    w.m = mx;
                 }
-            const typename S::Probs pr = S::probs(sc);
+                const float ref = w.m == -INFINITY ? 0.f : w.m;
+#pragma unroll
+                for (int x = 0; x < GROUPS; x++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        sc[rt][x][r] = fast_exp2((sc[rt][x][r] - ref) * kLog2e);
+                        w.l += sc[rt][x][r];
+                    }
+                pr[rt] = S::probs(sc[rt]);
+            }
             // ---- values ----
             // Values a row does not see may be anything (0 * inf is NaN), so around the last keys rows of different limits are
             // done one limit after the other, the largest first, with the values behind it cleared.
-            unsigned long long todo = whole ? ~0ull : __ballot(limit > k0);
-            bool mine = true;
-            while (todo != 0) {
-                if (whole) {
-                    todo = 0;
-                } else {
-                    const int sees = min(limit, k0 + KW);
-                    int cut = todo >> lane & 1 ? sees : 0;
+            unsigned long long todo[RT], any = 0;
+            bool mine[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) {
+                todo[rt] = whole ? ~0ull : __ballot(row[rt].limit > k0);
+                mine[rt] = true;
+                any |= todo[rt];
+            }
+            while (any != 0) {
+                any = 0;
+                if (!whole) {
+                    int cut = 0;
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) cut = max(cut, todo[rt] >> lane & 1 ? min(row[rt].limit, k0 + KW) : 0);
 #pragma unroll
                     for (int d = 1; d < 16; d *= 2) cut = max(cut, __shfl_xor(cut, d));
-                    mine = sees == cut;
-                    todo &= ~__ballot(mine);
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) {
+                        mine[rt] = min(row[rt].limit, k0 + KW) == cut;
+                        todo[rt] &= ~__ballot(mine[rt]);
+                        any |= todo[rt];
+                    }
 #pragma unroll
                     for (int x = 0; x < GROUPS; x++)
 #pragma unroll
@@ -599,45 +637,55 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void
                             if (k0 + 16 * x + 4 * g + r >= cut || !(held >> x & 1)) vr.x[x][r] = {};
                 }
 #pragma unroll
-                for (int t = 0; t < NV; t++) {
-                    const f32x4 d = S::product(vr, t, pr, o[t]);
+                for (int t = 0; t < NV; t++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) o[t][r] = mine ? d[r] : o[t][r];
-                }
+                    for (int rt = 0; rt < RT; rt++) {
+                        const f32x4 d = S::product(vr, t, pr[rt], row[rt].o[t]);
+#pragma unroll
+                        for (int r = 0; r < 4; r++) row[rt].o[t][r] = mine[rt] ? d[r] : row[rt].o[t][r];
+                    }
             }
         }
         if (more) load_values();
         if (have && k0 + STRIDE >= min(s.len, s.t1 * KW)) {
             // ---- a segment ends ----
-            l = column_sum(l);
-            if (limit <= 0) {                             // a row that sees nothing went along with the others
-                m = -INFINITY;
-                l = 0.f;
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) {
+                row[rt].l = column_sum(row[rt].l);
+                if (row[rt].limit <= 0) {                 // a row that sees nothing went along with the others
+                    row[rt].m = -INFINITY;
+                    row[rt].l = 0.f;
+                }
             }
             if constexpr (SPLIT) {
-                // The lane's channels of row i: 4 NV adjacent ones from 4 g NV on.
+                // The lane's channels of its row: 4 NV adjacent ones from 4 g NV on.
                 const bool all = s.t0 == 0 && s.t1 == s.n_steps;
-                if (all && has_row) {
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
-                    struct alignas(4 * NV * sizeof(T) < 16 ? 4 * NV * sizeof(T) : 16) Mine { T x[4 * NV]; } v;
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
+                for (int rt = 0; rt < RT; rt++) {
+                    const Row& w = row[rt];
+                    if (all && w.has) {
+                        const float inv = w.l == 0.f ? 0.f : 1.f / w.l;
+                        struct alignas(4 * NV * sizeof(T) < 16 ? 4 * NV * sizeof(T) : 16) Mine { T x[4 * NV]; } v;
 #pragma unroll
-                        for (int t = 0; t < NV; t++) v.x[r * NV + t] = (T)(l == 0.f ? 0.f : o[t][r] * inv);
-                    *(Mine*)((T*)p.out + (row_base + i) * C + 4 * g * NV) = v;
-                    if (g == 0) p.lse[row_base + i] = l == 0.f ? -INFINITY : m + __log2f(l) * kLn2;
-                }
-                if (!all && has_row) {
-                    const long long at = ((long long)worker * 2 + (s.t0 > 0 ? 0 : 1)) * min(kPaRows, rows_all) + i;
-                    struct alignas(16) Mine { float x[4 * NV]; } v;
+                        for (int r = 0; r < 4; r++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
+                            for (int t = 0; t < NV; t++) v.x[r * NV + t] = (T)(w.l == 0.f ? 0.f : w.o[t][r] * inv);
+                        const long long at = row_base + 16 * rt + i;
+                        *(Mine*)((T*)p.out + at * C + 4 * g * NV) = v;
+                        if (g == 0) p.lse[at] = w.l == 0.f ? -INFINITY : w.m + __log2f(w.l) * kLn2;
+                    }
+                    if (!all && w.has) {
+                        const long long at = ((long long)worker * 2 + (s.t0 > 0 ? 0 : 1)) * min(ROWS, rows_all) + 16 * rt + i;
+                        struct alignas(16) Mine { float x[4 * NV]; } v;
 #pragma unroll
-                        for (int t = 0; t < NV; t++) v.x[r * NV + t] = o[t][r];
-                    *(Mine*)(p.part_o + at * C + 4 * g * NV) = v;
-                    if (g == 0) {
-                        p.part_m[at] = m;
-                        p.part_l[at] = l;
+                        for (int r = 0; r < 4; r++)
+#pragma unroll
+                            for (int t = 0; t < NV; t++) v.x[r * NV + t] = w.o[t][r];
+                        *(Mine*)(p.part_o + at * C + 4 * g * NV) = v;
+                        if (g == 0) {
+                            p.part_m[at] = w.m;
+                            p.part_l[at] = w.l;
+                        }
                     }
                 }
                 // The group's first worker says who has the rest; a share that ends inside a group ends with its step t1.
@@ -655,19 +703,22 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C) : 2) void
                 // ---- the waves of the workgroup ----
                 extern __shared__ __align__(16) float sm_parts[];
                 constexpr int PITCH = C + 4;                              // rows start in different banks
-                const int part_rows = min(kPaRows, rows_all);
+                const int part_rows = min(ROWS, rows_all);
                 float* sm_m = sm_parts + W * part_rows * PITCH;
                 float* sm_l = sm_m + W * part_rows;
-                if (has_row) {
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
+                for (int rt = 0; rt < RT; rt++)
+                    if (row[rt].has) {
+                        const int at = wave * part_rows + 16 * rt + i;
 #pragma unroll
-                        for (int t = 0; t < NV; t++) sm_parts[(wave * part_rows + i) * PITCH + (4 * g + r) * NV + t] = o[t][r];
-                    if (g == 0) {
-                        sm_m[wave * part_rows + i] = m;
-                        sm_l[wave * part_rows + i] = l;
+                        for (int r = 0; r < 4; r++)
+#pragma unroll
+                            for (int t = 0; t < NV; t++) sm_parts[at * PITCH + (4 * g + r) * NV + t] = row[rt].o[t][r];
+                        if (g == 0) {
+                            sm_m[at] = row[rt].m;
+                            sm_l[at] = row[rt].l;
+                        }
                     }
-                }
                 __syncthreads();
                 for (int x = tid; x < rows * (C / 4); x += pa_threads(W)) {
                     const int r = x / (C / 4), c4 = x % (C / 4);
@@ -706,7 +757,7 @@ __global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, in
     const int r = blockIdx.y * (SL / lanes) + slot / lanes;
     if (more == 0) return;                                // (uniform)
     const bool has_row = r < join.w;
-    const int part_rows = min(kPaRows, p.G * p.N);
+    const int part_rows = min(p.tile_rows, p.G * p.N);
     auto part = [&](int k) { return ((long long)(first + k) * 2 + (k == 0 ? 1 : 0)) * part_rows + (has_row ? r : 0); };
 
     // the slot's parts, and then the slots', each by the running maximum
@@ -758,33 +809,40 @@ __global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, in
         for (int e = 0; e < 4; e++) ot[e] = fmaf(w, x[e], ot[e]);
     }
     const int b = join.z / (p.Hkv * p.row_tiles), grp = join.z - b * p.Hkv * p.row_tiles;
-    const int h = grp / p.row_tiles, r0 = (grp - h * p.row_tiles) * kPaRows;
+    const int h = grp / p.row_tiles, r0 = (grp - h * p.row_tiles) * p.tile_rows;
     write_row<T, C>(p, (long long)b * p.H * p.N + (long long)h * (p.G * p.N) + r0 + r, c4, ot, lt, mx);
 }
 
-template <typename T, int C, int BIAS, bool PF32, int W>
+template <typename T, int C, int BIAS, bool PF32, int W, int RT>
 int launch_groups(const PagedAttnParams& p, hipStream_t stream) {
     const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;
     if (blocks >= (1LL << 31)) return -1;
-    const int rows = p.G * p.N < kPaRows ? p.G * p.N : kPaRows;
-    if constexpr (group_lds(W, kPaRows, C) > 65536) {
+    const int rows = p.G * p.N < 16 * RT ? p.G * p.N : 16 * RT;
+    if constexpr (group_lds(W, 16 * RT, C) > 65536) {
         static FbLdsOnce once;
-        if (!fb_raise_lds_limit((const void*)paged_attn_kernel<T, C, BIAS, PF32, W>, group_lds(W, kPaRows, C), once)) return 1;
+        if (!fb_raise_lds_limit((const void*)paged_attn_kernel<T, C, BIAS, PF32, W, RT>, group_lds(W, 16 * RT, C), once)) return 1;
     }
-    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, W>), dim3((unsigned)blocks), dim3(pa_threads(W)), group_lds(W, rows, C), stream, p);
+    const size_t lds = group_lds(W, rows, C);
+    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, W, RT>), dim3((unsigned)blocks), dim3(pa_threads(W)), lds, stream, p);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
 template <typename T, int C, int BIAS, bool PF32>
 int launch_attn(const PagedAttnParams& p, hipStream_t stream) {
     if (p.workers == 0) {
-        return p.waves == 8 ? launch_groups<T, C, BIAS, PF32, 8>(p, stream) : launch_groups<T, C, BIAS, PF32, 4>(p, stream);
+        if constexpr (two_tiles(C, std::is_same_v<T, float>)) {
+            if (p.tile_rows == 32) return launch_groups<T, C, BIAS, PF32, 4, 2>(p, stream);
+        }
+        return p.waves == 8 ? launch_groups<T, C, BIAS, PF32, 8, 1>(p, stream) : launch_groups<T, C, BIAS, PF32, 4, 1>(p, stream);
     }
-    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, 1>), dim3((unsigned)((p.workers + kPaWaves - 1) / kPaWaves)), dim3(kPaThreads), 0,
-                       stream, p);
+    const dim3 blocks((unsigned)((p.workers + kPaWaves - 1) / kPaWaves));
+    if constexpr (two_tiles(C, std::is_same_v<T, float>)) {
+        if (p.tile_rows == 32) hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, 1, 2>), blocks, dim3(kPaThreads), 0, stream, p);
+    }
+    if (p.tile_rows == 16) hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, 1, 1>), blocks, dim3(kPaThreads), 0, stream, p);
     if (hipGetLastError() != hipSuccess) return 1;
     const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
-    const int rows = p.G * p.N < kPaRows ? p.G * p.N : kPaRows;
+    const int rows = p.G * p.N < p.tile_rows ? p.G * p.N : p.tile_rows;
     // slots: as many parts at a time as a group has on average, the rest are rows
     const long long parts = p.workers / groups;
     const int lanes = parts >= 6 ? 8 : (parts >= 3 ? 4 : 2);
@@ -823,29 +881,47 @@ int attn_channels(const PagedAttnParams& p, int C, hipStream_t stream) {
 
 }  // namespace
 
+// rows: query rows of a key head
+static size_t parts_of(int workers, long long rows, int tile_rows) {
+    return (size_t)workers * 2 * (rows < tile_rows ? rows : tile_rows);
+}
+
 // Waves that share the keys: all that are resident.  Short requests (by the table's width) are not split: a turn of a workgroup's
 // waves takes a memory latency, 1.2 us at C = 64 and 1.7 at 128, the split's bookkeeping, its join and the launch of
 // that 5 us on either side of the queue.  us without / with the split, on the GPU; as calls one after the other:
 //   bf16 C 64, 16 groups 1024 keys 10.6 / 11.0; 11.6 / 16.5, 1536 keys 16.5 / 11.2; 15.7 / 16.2; 1024 groups 1024 keys 46 / 50; 44 / 50
 //   bf16 C 128, 16 groups 640 keys 11.6 / 13.0; 11.4 / 16.2, 1024 keys 16.8 / 13.2; 16.2 / 16.2
 //   fp32 C 64, 16 groups 512 keys 11.2 / 11.2; 11.7 / 16.3, 768 keys 16.0 / 11.4; 15.4 / 16.5; C 128 320 keys 12.6 / 14.3; 11.7 / 16.1
-int fb_paged_attn_workers(int B, int Hkv, int row_tiles, long long capacity, int C, bool f32) {
+//
+// Two tiles of 16 rows read a key once, for a longer step and twice the parts.  That pays where the loads bound the call: in bf16 at
+// 64 and 128 channels (fp32 is bound by its matrix products, 16 and 32 channels by the softmax: N 20, B 8, H 16, C 16 31.2 / 35.4 us
+// with 16 / 32 rows, C 32 38.4 / 38.8; B 32, H 8 / 4, fp32 C 64 83 / 96), and from 12 steps a wave on or, without a split, three groups
+// per CU of more than two turns.  us with 16 / 32 rows, N 20, H = Hkv = 16:
+//   up to 8200 keys, C 128: B 1 36 / 42, 2 39 / 43, 3 50 / 49, 4 58 / 53, 8 99 / 73, with 64 rows 173 / 128; C 64: B 2 27 / 31, 4 37 / 36,
+//   6 44 / 41, 8 54 / 47
+//   no split, C 128, 300 keys: B 8 16 / 23, 16 23 / 24, 24 33 / 28, 128 132 / 108; C 64, 1024 keys: B 16 30 / 29, 32 49 / 37; 112 keys: B 64
+//   28 / 31
+PagedAttnSplit fb_paged_attn_split(int B, int Hkv, long long rows, long long capacity, int C, bool f32) {
+    PagedAttnSplit s;
     const int step = 16 * step_groups(C, f32);
     const long long steps = (capacity + step - 1) / step;
-    if (capacity <= (C == 128 ? 640 : 1024) / (f32 ? 2 : 1)) return 0;
     int cus = fb_cu_count();
     if (cus <= 0) cus = 256;
-    const long long groups = (long long)B * Hkv * row_tiles;
-    if ((steps + kPaLead) * groups >= (1LL << 31)) return 0;         // costs are counted in 32 bits
-    const long long most = groups * ((steps + kPaLeast - 1) / kPaLeast), all = 4LL * waves_per_simd(C) * cus;
-    return (int)(most < all ? most : all);
-}
-
-// rows: query rows of a key head
-static size_t parts_of(int workers, long long rows) { return (size_t)workers * 2 * (rows < kPaRows ? rows : kPaRows); }
-
-size_t fb_paged_attn_workspace_bytes(int workers, long long groups, long long rows, int C) {
-    return parts_of(workers, rows) * (C + 2) * sizeof(float) + (size_t)(groups < workers ? groups : workers) * sizeof(int4);
+    long long groups = (long long)B * Hkv * ((rows + 15) / 16);
+    // (costs are counted in 32 bits)
+    const bool split = capacity > (C == 128 ? 640 : 1024) / (f32 ? 2 : 1) && steps + kPaLead < (1LL << 31) / groups;
+    const bool large = split ? steps * groups >= 12LL * 4 * waves_per_simd(C, 1) * cus : groups >= 3LL * cus && capacity > 2 * 4 * step;
+    s.tile_rows = rows > 16 && two_tiles(C, f32) && large ? 32 : 16;
+    s.row_tiles = (int)((rows + s.tile_rows - 1) / s.tile_rows);
+    groups = (long long)B * Hkv * s.row_tiles;
+    const long long most = groups * ((steps + kPaLeast - 1) / kPaLeast), all = 4LL * waves_per_simd(C, s.tile_rows / 16) * cus;
+    s.workers = !split ? 0 : (int)(most < all ? most : all);
+    s.bytes = 0;
+    if (split) {
+        const size_t joins = (size_t)(groups < s.workers ? groups : s.workers);
+        s.bytes = parts_of(s.workers, rows, s.tile_rows) * (C + 2) * sizeof(float) + joins * sizeof(int4);
+    }
+    return s;
 }
 
 int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream_t stream) {
@@ -855,7 +931,7 @@ int fb_launch_paged_attn(PagedAttnParams p, int C, bool f32, void* ws, hipStream
     p.capacity = capacity < 0x7fffff00 ? (int)capacity : 0x7fffff00;
     if (p.workers) {
         const long long groups = (long long)p.B * p.Hkv * p.row_tiles;
-        const size_t parts = parts_of(p.workers, (long long)p.G * p.N);
+        const size_t parts = parts_of(p.workers, (long long)p.G * p.N, p.tile_rows);
         p.joins_by_group = groups <= p.workers;
         p.joins = (int4*)ws;
         p.part_o = (float*)(p.joins + (p.joins_by_group ? groups : p.workers));

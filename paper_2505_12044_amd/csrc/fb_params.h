@@ -122,13 +122,13 @@ struct PagedAttnParams {
     long long phiq_bstride;
     int B, H, Hkv, N, R, page_shift, n_pages, max_blocks, causal, phi_f32;
     float scale;
-    int row_tiles;           // query rows of a key head (H / Hkv * N of them, below 2^24) in tiles of 16
+    int tile_rows, row_tiles;    // query rows of a key head (H / Hkv * N of them, below 2^24) in tiles of 16 or 32
     int G, capacity;         // set by the launch: H / Hkv; keys that a table row has room for
     float inv_n;             // 1 / N
     int workers;             // waves the keys are split over; 0: a workgroup per key head and row tile, no split
     int waves;               // of such a workgroup, set by the launch
     int joins_by_group;      // joins has an entry per (request, key head, row tile), else one per worker
-    float* part_o;           // scratch: two parts per worker, [workers, 2, rows, C], rows = min(16, H / Hkv * N)
+    float* part_o;           // scratch: two parts per worker, [workers, 2, rows, C], rows = min(tile_rows, H / Hkv * N)
     float* part_m;           // [workers, 2, rows] maxima
     float* part_l;           // [workers, 2, rows] sums
     int4* joins;             // workers behind the first that have parts (0: no join), the first, the group, its rows

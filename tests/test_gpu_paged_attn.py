@@ -278,3 +278,66 @@ def test_lengths_in_a_wide_table(length):
 def test_numbers_of_requests(B):
     rng = np.random.default_rng(B)
     run(B, 1, 2, 1, 32, 16, rng.integers(0, 200, B), BF, "alibi", room=200, seed=B)
+
+
+# More than 16 query rows a key head in calls large enough (by the table's width, or in number) that two tiles share a step.
+WIDE = 400                                                               # blocks of 256 keys
+
+
+@pytest.mark.parametrize("C", [64, 128])
+@pytest.mark.parametrize("bias,R,phi", [("none", 0, F32), ("alibi", 0, F32), ("factors", 2, F32), ("factors", 3, BF), ("factors", 8, F32),
+                                        ("factors", 16, BF), ("factors", 21, F32)])
+def test_two_row_tiles(C, bias, R, phi):
+    run(3, 5, 8, 2, C, 256, [5, 300, 1031], BF, bias, R, phi, room=WIDE)
+    run(3, 5, 8, 2, C, 256, [5, 300, 1031], BF, bias, R, phi, room=WIDE, workspace="none")
+
+
+@pytest.mark.parametrize("H,Hkv,N", [(2, 2, 17), (2, 2, 31), (2, 2, 32), (2, 2, 33), (2, 2, 64), (34, 2, 1), (66, 2, 1), (20, 2, 7)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_of_two_tiles(H, Hkv, N, causal):
+    run(4, N, H, Hkv, 64, 256, [0, 1, 70, 611], BF, "alibi", causal=causal, room=WIDE)
+    run(3, N, H, Hkv, 128, 256, [N, 33, 257], BF, "none", causal=causal, room=WIDE)
+
+
+@pytest.mark.parametrize("C", [64, 128])
+def test_queries_outside_their_request_in_two_tiles(C):
+    run(7, 20, 4, 2, C, 256, [0, 3, 20, 517, 1, 40, 300], BF, "alibi", starts=[0, 0, 18, 500, 25, -2, -24], room=WIDE)
+    run(4, 20, 4, 2, C, 256, [0, 2, 9, 1000], BF, "factors", 2, room=WIDE)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_two_tiles_and_entries_that_are_no_pages(causal):
+    lens = [900, 64, 33]
+    c = make_cache(lens, 2, 16, 64, 0, BF, F32, 5, extra_blocks=16 * WIDE)
+    q = randn(torch.Generator().manual_seed(8), (3, 4, 10, 64), BF)
+    good = c["table"].clone()
+    hide = [torch.zeros(max(lens), dtype=torch.bool) for _ in lens]
+    for b, j, entry in ((0, 0, -1), (0, 7, 1 << 30), (0, 8, c["k_pages"].shape[0]), (0, 56, -(1 << 31)), (2, 0, -1), (2, 1, -7), (2, 2, -1)):
+        c["table"][b, j] = entry
+        hide[b][16 * j:16 * j + 16] = True
+    got = api.fb_paged_attn_fwd(q, c["k_pages"], c["v_pages"], c["table"], c["lens"], causal=causal)
+    torch.cuda.synchronize()
+    c["table"] = good
+    check_attend(got, attend64(q, c, causal=causal, hide=hide))
+
+
+@pytest.mark.parametrize("C", [64, 128])
+@pytest.mark.parametrize("G,N", [(2, 9), (1, 32), (3, 11)])
+def test_two_tiles_of_many_short_requests(C, G, N):
+    lens = np.random.default_rng(C + N).integers(0, 330, 130)
+    run(130, N, 3 * G, 3, C, 16, lens, BF, "alibi", room=16)
+
+
+def test_two_tiles_give_the_same_bits_and_long_requests():
+    rng = np.random.default_rng(2)
+    lens = rng.integers(1000, 9000, 8)
+    c = make_cache(lens, 16, 64, 128, 0, BF, F32, 3)
+    q = randn(torch.Generator().manual_seed(8), (8, 16, 18, 128), BF)
+    first = api.fb_paged_attn_fwd(q, c["k_pages"], c["v_pages"], c["table"], c["lens"])
+    torch.cuda.synchronize()
+    for _ in range(2):
+        again = api.fb_paged_attn_fwd(q, c["k_pages"], c["v_pages"], c["table"], c["lens"])
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    pick = 5                                                             # one request against the definition
+    one = {n: (x[pick:pick + 1] if n in ("table", "lens") else x) for n, x in c.items()}
+    check_attend((first[0][pick:pick + 1], first[1][pick:pick + 1]), attend64(q[pick:pick + 1], one))
