@@ -526,6 +526,15 @@ def _ints(name: str, t: torch.Tensor, *shape: int) -> int:
     return t.data_ptr()
 
 
+def _shared_factors(phi: torch.Tensor, B: int, flag: Optional[bool]) -> bool:
+    """Whether factors [B or 1, ...] are shared over the batch: their shape says so, and a flag that says otherwise is refused
+    (False for one set of factors would read past it, True for B sets would use the first for every request)."""
+    shared = phi.shape[0] == 1
+    if flag is not None and B > 1 and bool(flag) != shared:
+        raise FlashBiasError(f"phi_batch_broadcast={bool(flag)} contradicts factors of batch {phi.shape[0]} in a batch of {B}")
+    return shared and B > 1
+
+
 _Six = ctypes.c_longlong * 6
 
 
@@ -634,9 +643,11 @@ def _check_pages(k_pages, v_pages, phi_pages, factors):
 def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, phi_batch_broadcast: Optional[bool] = None,
                     stream=None) -> None:
     """Stores k, v [B,Hkv,N,C] (any strides with adjacent channels) and phi_k [B or 1,Hkv,N,R] in the rows slots [B,N] of
-    k_pages, v_pages [n_pages,Hkv,page,C] and phi_pages [n_pages,Hkv,page,R].  Slots of -1 are left out; the others must differ."""
+    k_pages, v_pages [n_pages,Hkv,page,C] and phi_pages [n_pages,Hkv,page,R].  Slots of -1 are left out; the others must differ.
+    phi_batch_broadcast follows from phi_k's shape; a value that contradicts it is refused."""
     lib = load_library()
     strides = _row_strides(k, v)
+    shared = phi_k is not None and _shared_factors(phi_k, k.shape[0], phi_batch_broadcast)
     handle = _here(stream, k, v, slots, k_pages, v_pages, phi_k, phi_pages)
     B, Hkv, N, C = k.shape
     n_pages, hp, page, cp, R = _check_pages(k_pages, v_pages, phi_pages, phi_k)
@@ -646,11 +657,8 @@ def fb_paged_append(k, v, slots, k_pages, v_pages, phi_k=None, phi_pages=None, p
     if R:
         _need(phi_k.shape == (B, Hkv, N, R) or phi_k.shape == (1, Hkv, N, R), "phi_k must be [B or 1,Hkv,N,R]")
         phi_code = _dtype_code(phi_k)
-        if phi_batch_broadcast is None:
-            phi_batch_broadcast = phi_k.shape[0] == 1 and B > 1
     st = lib.fb_paged_append(k.data_ptr(), v.data_ptr(), _ptr(phi_k), _ints("slots", slots, B, N), _ptr(k_pages), _ptr(v_pages),
-                             _ptr(phi_pages), strides, B, Hkv, N, C, R, page, n_pages, code, phi_code,
-                             bool(phi_batch_broadcast), handle)
+                             _ptr(phi_pages), strides, B, Hkv, N, C, R, page, n_pages, code, phi_code, shared, handle)
     _check(st, "fb_paged_append")
 
 
@@ -669,11 +677,13 @@ def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None,
                       phi_batch_broadcast: Optional[bool] = None, workspace=None, stream=None):
     """out, lse = attention of q [B,H,N,C], the N newest tokens of each request, over its pages: lens [B] keys each, the
     first new token at position starts[b] (None: lens - N).  k_pages, v_pages [n_pages,Hkv,page,C], H a multiple of Hkv.
-    Bias: phi_q [B or 1,H,N,R] with phi_pages [n_pages,Hkv,page,R], or slopes [H] (ALiBi), or none.  causal=False: every
+    Bias: phi_q [B or 1,H,N,R] with phi_pages [n_pages,Hkv,page,R] (phi_batch_broadcast follows from phi_q's shape; a value that
+    contradicts it is refused), or slopes [H] (ALiBi), or none.  causal=False: every
     query sees all keys (an encoder's states).  Queries that see nothing get out = 0, lse = -inf.  Scratch of
     fb_paged_attn_fwd_workspace_bytes: the caller's workspace, else the binding's own; a call that is given out and lse but no
     workspace allocates nothing and does without (a key head is then not split over the GPU)."""
     lib = load_library()
+    shared = phi_q is not None and _shared_factors(phi_q, q.shape[0], phi_batch_broadcast)
     handle = _here(stream, q, k_pages, v_pages, table, lens, starts, phi_q, phi_pages, slopes, out, lse, workspace)
     _need(q.dim() == 4 and table.dim() == 2, "q must be [B,H,N,C], table [B, max_blocks]")
     B, H, N, C = q.shape
@@ -684,8 +694,6 @@ def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None,
     if R:
         _need(phi_q.shape == (B, H, N, R) or phi_q.shape == (1, H, N, R), "phi_q must be [B or 1,H,N,R]")
         phi_code = _dtype_code(phi_q)
-        if phi_batch_broadcast is None:
-            phi_batch_broadcast = phi_q.shape[0] == 1 and B > 1
     if slopes is not None:
         _need(slopes.dtype is torch.float32 and slopes.numel() == H, "slopes must be a float32 tensor with one entry per head")
     ws_bytes = 0
@@ -706,6 +714,6 @@ def fb_paged_attn_fwd(q, k_pages, v_pages, table, lens, starts=None, phi_q=None,
     st = lib.fb_paged_attn_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(phi_q), _ptr(phi_pages), _ptr(slopes),
                                _ints("table", table, B, blocks), _ints("lens", lens, B), None if starts is None else _ints("starts", starts, B),
                                _ptr(out), _ptr(lse), B, H, Hkv, N, C, R, page, n_pages, blocks, bool(causal), code, phi_code,
-                               bool(phi_batch_broadcast), float(scale), _ptr(workspace), ws_bytes, handle)
+                               shared, float(scale), _ptr(workspace), ws_bytes, handle)
     _check(st, "fb_paged_attn_fwd")
     return out, lse
