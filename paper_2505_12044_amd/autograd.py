@@ -144,29 +144,47 @@ def _adjacent(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 
 
 class _Rotary(torch.autograd.Function):
-    """Rotary positions; the backward turns the gradients back and keeps nothing of q and k."""
+    """Rotary positions; the backward turns the gradients back and keeps nothing of q and k.  The map is linear, so its
+    backward is the same map with the other sign (inverse): where a graph of the gradients is wanted, the backward goes through
+    this function again.  q or k may be None."""
 
     @staticmethod
-    def forward(ctx, q, k, positions, freqs, sections, interleaved):
+    def forward(ctx, q, k, positions, freqs, sections, interleaved, inverse):
         ctx.save_for_backward(positions, freqs)
-        ctx.cfg = (sections, interleaved)
-        yq, yk = api.fb_rotary_fwd(_adjacent(q), _adjacent(k), positions, freqs, sections, interleaved=interleaved)
-        return yq if yk is None else (yq, yk)
+        ctx.cfg = (sections, interleaved, inverse)
+        yq, yk = _turned(q, k, positions, freqs, sections, interleaved, inverse)
+        return yk if yq is None else (yq if yk is None else (yq, yk))
 
     @staticmethod
-    def backward(ctx, dq, dk=None):
+    def backward(ctx, *grads):
         positions, freqs = ctx.saved_tensors
-        sections, interleaved = ctx.cfg
-        dq, dk = api.fb_rotary_bwd(_adjacent(dq), _adjacent(dk), positions, freqs, sections, interleaved=interleaved)
-        return dq, dk, None, None, None, None
+        sections, interleaved, inverse = ctx.cfg
+        # gradients of the tensors that were given, and only those that are asked for
+        dq, dk = (grads if len(grads) == 2 else (grads[0], grads[0]))
+        dq, dk = (d if need else None for d, need in zip((dq, dk), ctx.needs_input_grad))
+        if torch.is_grad_enabled():
+            turned = _Rotary.apply(dq, dk, positions, freqs, sections, interleaved, not inverse)
+            dq, dk = turned if isinstance(turned, tuple) else (None if dq is None else turned, None if dk is None else turned)
+        else:
+            dq, dk = _turned(dq, dk, positions, freqs, sections, interleaved, not inverse)
+        return dq, dk, None, None, None, None, None
+
+
+def _turned(q, k, positions, freqs, sections, interleaved, inverse):
+    """The kernel's results for q and k; one of them may be None."""
+    turn = api.fb_rotary_bwd if inverse else api.fb_rotary_fwd
+    if q is None:
+        return None, turn(_adjacent(k), None, positions, freqs, sections, interleaved=interleaved)[0]
+    return turn(_adjacent(q), _adjacent(k), positions, freqs, sections, interleaved=interleaved)
 
 
 def rotary_positions(q, k, positions, freqs, sections, interleaved: bool = False):
     """q [B,H,N,C] and k [B,Hkv,N,C] (k may be None) turned by rotary positions of one to four axes; arguments as for
-    api.fb_rotary_fwd.  Differentiable in q and k; positions and freqs are constants.  Returns the pair (or q's alone)."""
+    api.fb_rotary_fwd.  Differentiable in q and k, any number of times; positions and freqs are constants.  Returns the pair
+    (or q's alone)."""
     if positions.requires_grad or freqs.requires_grad:
         raise api.FlashBiasError("positions and freqs are constants: they receive no gradient")
-    return _Rotary.apply(q, k, positions, freqs, tuple(sections), bool(interleaved))
+    return _Rotary.apply(q, k, positions, freqs, tuple(sections), bool(interleaved), False)
 
 
 def lowrank_bias_attention(q, k, v, phi_q=None, phi_k=None, causal: bool = False, scale: float = 0.0):
