@@ -14,6 +14,7 @@ There is no fallback path: without the shared library every call raises.
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional
 
 import torch
@@ -22,6 +23,7 @@ from . import api
 
 
 def _c(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """Contiguous, as the kernels take it.  In front of the functions, so that what they save is part of the graph."""
     return None if t is None else t.contiguous()
 
 
@@ -44,12 +46,36 @@ def _fold_pair(gq, like_q, gk, like_k):
     return _fold_batch(gq, like_q), _fold_batch(gk, like_k)
 
 
+class _FirstOnly(torch.autograd.Function):
+    """Gradients that the library cannot differentiate again, tied to the tensors they depend on."""
+
+    @staticmethod
+    def forward(ctx, compute, *depends_on):
+        return compute()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise api.FlashBiasError("the attention kernels have no second derivatives")
+
+
+def _first_only(backward):
+    """A backward whose gradients raise where they are differentiated again (create_graph=True), instead of leaving that
+    part of the second derivative out."""
+
+    @functools.wraps(backward)
+    def call(ctx, dout):
+        if not torch.is_grad_enabled():
+            return backward(ctx, dout)
+        return _FirstOnly.apply(lambda: backward(ctx, dout), dout, *ctx.saved_tensors)
+
+    return call
+
+
 class _LowRank(torch.autograd.Function):
     """softmax(q k^T scale + phi_q phi_k^T) v (Eq. 3); N queries, M keys (causal needs N = M)."""
 
     @staticmethod
     def forward(ctx, q, k, v, phi_q, phi_k, causal, scale):
-        q, k, v, phi_q, phi_k = _c(q), _c(k), _c(v), _c(phi_q), _c(phi_k)
         cross = q.shape[2] != k.shape[2]
         if cross:
             if causal:
@@ -62,6 +88,7 @@ class _LowRank(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_first_only
     def backward(ctx, dout):
         q, k, v, phi_q, phi_k, out, lse = ctx.saved_tensors
         causal, scale, cross = ctx.cfg
@@ -79,13 +106,13 @@ class _MulBias(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, phi_q, phi_k, causal, scale):
-        q, k, v, phi_q, phi_k = _c(q), _c(k), _c(v), _c(phi_q), _c(phi_k)
         out, lse = api.fb_lowrank_mulbias_attn_fwd(q, k, v, phi_q, phi_k, causal=causal, scale=scale)
         ctx.save_for_backward(q, k, v, phi_q, phi_k, out, lse)
         ctx.cfg = (bool(causal), float(scale))
         return out
 
     @staticmethod
+    @_first_only
     def backward(ctx, dout):
         q, k, v, phi_q, phi_k, out, lse = ctx.saved_tensors
         causal, scale = ctx.cfg
@@ -99,13 +126,13 @@ class _Alibi(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, slopes, causal, scale):
-        q, k, v, slopes = _c(q), _c(k), _c(v), _c(slopes)
         out, lse = api.fb_alibi_attn_fwd(q, k, v, slopes, causal=causal, scale=scale)
         ctx.save_for_backward(q, k, v, slopes, out, lse)
         ctx.cfg = (bool(causal), float(scale))
         return out
 
     @staticmethod
+    @_first_only
     def backward(ctx, dout):
         q, k, v, slopes, out, lse = ctx.saved_tensors
         causal, scale = ctx.cfg
@@ -123,13 +150,13 @@ class _DenseBias(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, v, bias, causal, scale):
-        q, k, v, bias = _c(q), _c(k), _c(v), _c(bias)
         out, lse = api.fb_dense_bias_attn_fwd(q, k, v, bias, causal=causal, scale=scale)
         ctx.save_for_backward(q, k, v, bias, out, lse)
         ctx.cfg = (bool(causal), float(scale))
         return out
 
     @staticmethod
+    @_first_only
     def backward(ctx, dout):
         q, k, v, bias, out, lse = ctx.saved_tensors
         causal, scale = ctx.cfg
@@ -190,19 +217,19 @@ def rotary_positions(q, k, positions, freqs, sections, interleaved: bool = False
 def lowrank_bias_attention(q, k, v, phi_q=None, phi_k=None, causal: bool = False, scale: float = 0.0):
     """Attention with the additive bias phi_q phi_k^T.  q [B,H,N,C]; k, v [B,H,M,C]; phi_q [B or 1,H,N,R];
     phi_k [B or 1,H,M,R]; scale 0 means 1/sqrt(C).  Differentiable in q, k, v, phi_q, phi_k."""
-    return _LowRank.apply(q, k, v, phi_q, phi_k, causal, scale)
+    return _LowRank.apply(_c(q), _c(k), _c(v), _c(phi_q), _c(phi_k), causal, scale)
 
 
 def multiplicative_bias_attention(q, k, v, phi_q, phi_k, causal: bool = False, scale: float = 0.0):
     """Attention whose scores are multiplied by phi_q phi_k^T.  Differentiable in all five tensors."""
-    return _MulBias.apply(q, k, v, phi_q, phi_k, causal, scale)
+    return _MulBias.apply(_c(q), _c(k), _c(v), _c(phi_q), _c(phi_k), causal, scale)
 
 
 def alibi_attention(q, k, v, slopes, causal: bool = True, scale: float = 0.0):
     """Attention with the ALiBi bias -slopes[h] (i - j); slopes: [H] float32.  Differentiable in q, k, v, slopes."""
-    return _Alibi.apply(q, k, v, slopes, causal, scale)
+    return _Alibi.apply(_c(q), _c(k), _c(v), _c(slopes), causal, scale)
 
 
 def dense_bias_attention(q, k, v, bias, causal: bool = False, scale: float = 0.0):
     """Attention with a materialised bias [B or 1,H,N,N] of q's dtype.  Differentiable in q, k, v, bias."""
-    return _DenseBias.apply(q, k, v, bias, causal, scale)
+    return _DenseBias.apply(_c(q), _c(k), _c(v), _c(bias), causal, scale)
