@@ -605,7 +605,14 @@ def fb_paged_plan(lens, new_lens, table, ring, state, n_new: int, page: int, len
     """Moves B requests from lens to new_lens tokens: pages are given back and taken (table [B, max_blocks] and the ring of
     free pages, int32, in place), and the up to n_new new tokens of each are mapped.  Returns lens [B] and state [2]
     (ring head, free pages) afterwards, slots [B, n_new] (-1: no token) and positions [B, n_new]."""
-    lib = load_library()
+    args, out = _plan_call(lens, new_lens, table, ring, state, n_new, page, lens_out, state_out, slots, positions, stream)
+    _run_plan(args)
+    return out
+
+
+def _plan_call(lens, new_lens, table, ring, state, n_new, page, lens_out=None, state_out=None, slots=None, positions=None,
+               stream=None):
+    """The checked arguments of the entry point, and the tensors it writes."""
     handle = _here(stream, lens, new_lens, table, ring, state, lens_out, state_out, slots, positions)
     _need(lens.dim() == 1 and table.dim() == 2 and ring.dim() == 1, "lens, ring: one dimension, table: [B, max_blocks]")
     B, blocks, n_pages = lens.shape[0], table.shape[1], ring.shape[0]
@@ -618,12 +625,14 @@ def fb_paged_plan(lens, new_lens, table, ring, state, n_new: int, page: int, len
         slots = new((B, n_new))
     if positions is None:
         positions = new((B, n_new))
-    st = lib.fb_paged_plan(_ints("lens", lens, B), _ints("new_lens", new_lens, B), _ints("table", table, B, blocks),
-                           _ints("ring", ring, n_pages), _ints("state", state, 2), _ints("lens_out", lens_out, B),
-                           _ints("state_out", state_out, 2), _ints("slots", slots, B, n_new), _ints("positions", positions, B, n_new),
-                           B, n_new, page, n_pages, blocks, handle)
-    _check(st, "fb_paged_plan")
-    return lens_out, state_out, slots, positions
+    return ((_ints("lens", lens, B), _ints("new_lens", new_lens, B), _ints("table", table, B, blocks), _ints("ring", ring, n_pages),
+             _ints("state", state, 2), _ints("lens_out", lens_out, B), _ints("state_out", state_out, 2),
+             _ints("slots", slots, B, n_new), _ints("positions", positions, B, n_new), B, n_new, page, n_pages, blocks, handle),
+            (lens_out, state_out, slots, positions))
+
+
+def _run_plan(args) -> None:
+    _check(load_library().fb_paged_plan(*args), "fb_paged_plan")
 
 
 def _check_pages(k_pages, v_pages, phi_pages, factors):

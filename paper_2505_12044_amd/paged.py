@@ -30,12 +30,15 @@ class PagedCache:
             raise api.FlashBiasError("sizes must be positive")
         if page not in (16, 32, 64, 128, 256):
             raise api.FlashBiasError("page must be 16, 32, 64, 128 or 256")
+        blocks = -(-max_tokens // page)
+        if requests > 4096 or n_pages * page >= 1 << 31 or requests * blocks >= 1 << 31:
+            raise api.FlashBiasError("at most 4096 requests, and fewer than 2^31 tokens and table entries")
         self.page = page
         shape = (layers, n_pages, kv_heads, page)
         self.k_pages = torch.empty((*shape, head_dim), dtype=dtype, device=device)
         self.v_pages = torch.empty((*shape, head_dim), dtype=dtype, device=device)
         self.phi_pages = torch.empty((*shape, rank), dtype=phi_dtype, device=device) if rank else None
-        self.table = torch.full((requests, -(-max_tokens // page)), -1, dtype=torch.int32, device=device)
+        self.table = torch.full((requests, blocks), -1, dtype=torch.int32, device=device)
         self.ring = torch.arange(n_pages, dtype=torch.int32, device=device)
         # lengths and the ring's (head, count), now and before the step
         self._now = torch.zeros(requests + 2, dtype=torch.int32, device=device)
@@ -47,11 +50,15 @@ class PagedCache:
 
     def step(self, new_lens: torch.Tensor, n_new: int) -> None:
         """From lens to new_lens, at most n_new new tokens a request: sets starts (the lengths before), lens, slots and
-        positions [requests, n_new]."""
+        positions [requests, n_new].  A step that is refused (it raises) leaves everything as it was."""
         b = self.table.shape[0]
+        if not 1 <= n_new < (1 << 31) // b:
+            raise api.FlashBiasError("n_new must be at least 1, and requests * n_new below 2^31")
+        args, out = api._plan_call(self.starts, new_lens, self.table, self.ring, self._before[b:], n_new, self.page, self.lens,
+                                   self._now[b:])
         self._before.copy_(self._now)
-        _, _, self.slots, self.positions = api.fb_paged_plan(
-            self.starts, new_lens, self.table, self.ring, self._before[b:], n_new, self.page, self.lens, self._now[b:])
+        api._run_plan(args)
+        _, _, self.slots, self.positions = out
 
     def _layer_factors(self, layer: int):
         return None if self.phi_pages is None else self.phi_pages[layer]
