@@ -384,7 +384,7 @@ int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* 
  * or ALiBi -slopes[h] (i - j) (slopes [H] float, R = 0; exact below 2^24 positions), or none.
  *   Query n of request b has the position i = starts[b] + n (starts NULL: lens[b] - N + n).  causal: it sees the keys
  *   j <= i of the request and is no query at all when i lies outside [0, lens[b]); else it sees all lens[b] keys (states of an
- *   encoder).  Keys in a table entry that is no page are not seen; lens are cut to [0, max_blocks * page].  What lies in the pages behind the
+ *   encoder).  Keys in a table entry that is no page are not seen; lens are cut to [0, max_blocks * page], and to 2^31 - 256.  What lies in the pages behind the
  *   last token, or in rows a query does not see, never reaches the result.  A query that sees nothing, or scores of -infinity
  *   only, has out = 0 and lse = -infinity.
  *   N is meant to be small: every 16 or 32 of a key head's H / Hkv * N query rows read its keys again (H / Hkv * N < 2^24).

@@ -202,6 +202,10 @@ FB_DEV ConstInts const_ints(const int* x) { return (ConstInts)(uintptr_t)x; }
 // Keys of a request: its length within the table (capacity: 31 bits).
 FB_DEV int held_keys(const PagedAttnParams& p, int len) { return max(min(len, p.capacity), 0); }
 
+// Whether k + stride lies below end; their sum may pass 31 bits.
+constexpr bool goes_on(int k, int stride, int end) { return k < end - stride; }
+static_assert(goes_on(64, 512, 577) && !goes_on(64, 512, 576) && !goes_on(0, 512, 0) && !goes_on(0x7ffffe80, 512, 0x7fffff00), "");
+
 // Steps of a request per group; one that holds nothing has one too (its rows are written).
 template <int KW>
 FB_DEV int steps_of(int len) { return len > KW ? (int)((unsigned)(len + KW - 1) / KW) : 1; }
@@ -496,7 +500,7 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C, RT) : 2) 
 #pragma unroll
         for (int x = 0; x < GROUPS; x++) page[x] = f_page[x];
         have = true;
-        if (fk + STRIDE < min(f.len, f.t1 * KW)) {
+        if (goes_on(fk, STRIDE, min(f.len, f.t1 * KW))) {
             fk += STRIDE;
         } else if (SPLIT && left > kPaLead) {
             if (++f.grp == groups) {
@@ -647,7 +651,7 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C, RT) : 2) 
             }
         }
         if (more) load_values();
-        if (have && k0 + STRIDE >= min(s.len, s.t1 * KW)) {
+        if (have && !goes_on(k0, STRIDE, min(s.len, s.t1 * KW))) {
             // ---- a segment ends ----
 #pragma unroll
             for (int rt = 0; rt < RT; rt++) {
