@@ -650,8 +650,7 @@ static int rotary_impl(const void* x0, void* y0, int H0, const void* x1, void* y
     p.end0 = sections[0]; p.end1 = p.end0 + sections[1]; p.end2 = p.end1 + sections[2];
     p.pos_f32 = positions_f32 != 0; p.pos_shared = positions_shared != 0; p.interleaved = interleaved != 0;
     p.inverse = inverse;
-    const int rc = fb_launch_rotary(p, dtype == FB_F32, (hipStream_t)stream);
-    return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
+    return fb_launch_rotary(p, dtype == FB_F32, (hipStream_t)stream) == 0 ? FB_OK : FB_ERR_LAUNCH;
 }
 
 int fb_rotary_fwd(const void* x0, void* y0, int H0, const void* x1, void* y1, int H1, const long long* strides,
@@ -723,8 +722,7 @@ int fb_paged_append(const void* k, const void* v, const void* phi_k, const int* 
     p.phi_k = phi_k; p.phik_bstride = phi_batch_broadcast ? 0 : (long long)Hkv * N * R;
     p.slots = slots; p.k_pages = k_pages; p.v_pages = v_pages; p.phi_pages = phi_pages;
     p.B = B; p.Hkv = Hkv; p.N = N; p.C = C; p.R = R; p.page_shift = page_shift_of(page); p.n_pages = n_pages;
-    const int rc = fb_launch_paged_append(p, dtype == FB_F32, phi_dtype == FB_F32, (hipStream_t)stream);
-    return rc == 0 ? FB_OK : (rc < 0 ? FB_ERR_SHAPE : FB_ERR_LAUNCH);
+    return fb_launch_paged_append(p, dtype == FB_F32, phi_dtype == FB_F32, (hipStream_t)stream) == 0 ? FB_OK : FB_ERR_LAUNCH;
 }
 
 static PagedAttnSplit paged_split(int B, int H, int Hkv, int N, int C, int page, int max_blocks, fb_dtype dtype) {

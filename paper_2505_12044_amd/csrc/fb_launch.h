@@ -57,6 +57,10 @@ int fb_launch_mulbias_fold(const void* x, const void* phi, const void* g_head, c
 int fb_launch_fold_batch(const void* s0, void* d0, long long n0, const void* s1, void* d1, long long n1, int B, bool f32,
                          hipStream_t stream);
 
+// A launch takes fewer than 2^32 threads.  Rotary positions, cache pages and attention over them send larger grids in parts
+// of so many workgroups (of up to 512 threads), each long enough that the gap between them does not show.
+constexpr long long kFbLaunchBlocks = 1LL << 22;
+
 // Rotary positions.
 int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream);
 

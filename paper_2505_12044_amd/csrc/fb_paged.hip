@@ -1,6 +1,8 @@
 // Pages of a key-value cache: which request owns which page, and the new tokens' rows stored into them.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "fb_device.h"
 #include "fb_launch.h"
 #include "fb_params.h"
@@ -183,7 +185,7 @@ template <typename V, int SIZE>
 __global__ __launch_bounds__(kAppThreads) void paged_append_kernel(PagedAppendParams p, int phi_size) {
     constexpr int VEC = sizeof(V) / SIZE;               // elements of a vector
     const int units = p.C / VEC;
-    const long long id = (long long)blockIdx.x * kAppThreads + threadIdx.x;
+    const long long id = (p.block0 + blockIdx.x) * kAppThreads + threadIdx.x;
     const long long token = id / units;
     const int u = (int)(id - token * units);
     if (token >= (long long)p.B * p.N) return;
@@ -225,12 +227,13 @@ template <typename V, int SIZE>
 int launch_append(PagedAppendParams& p, int phi_size, hipStream_t stream) {
     const long long threads = (long long)p.B * p.N * (p.C / (int)(sizeof(V) / SIZE));
     const long long blocks = (threads + kAppThreads - 1) / kAppThreads;
-    if (blocks >= (1LL << 31)) return -1;
     long long groups = (512 + blocks - 1) / blocks;     // heads per thread: as many as leave 512 workgroups
     if (groups > p.Hkv) groups = p.Hkv;
     p.heads_per_group = (int)((p.Hkv + groups - 1) / groups);
     groups = (p.Hkv + p.heads_per_group - 1) / p.heads_per_group;
-    hipLaunchKernelGGL((paged_append_kernel<V, SIZE>), dim3((unsigned)blocks, (unsigned)groups), dim3(kAppThreads), 0, stream, p, phi_size);
+    for (p.block0 = 0; p.block0 < blocks; p.block0 += kFbLaunchBlocks)
+        hipLaunchKernelGGL((paged_append_kernel<V, SIZE>), dim3((unsigned)std::min(blocks - p.block0, kFbLaunchBlocks), (unsigned)groups),
+                           dim3(kAppThreads), 0, stream, p, phi_size);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

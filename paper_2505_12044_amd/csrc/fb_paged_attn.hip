@@ -21,6 +21,7 @@
 // where no request can be long, a workgroup's waves share one group and join through LDS.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "fb_device.h"
@@ -370,8 +371,9 @@ __global__ __launch_bounds__(pa_threads(W), W == 1 ? waves_per_simd(C, RT) : 2) 
             return;
         }
     } else {
-        f.b = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)groups);
-        f.grp = blockIdx.x - f.b * groups;
+        const unsigned block = p.block0 + blockIdx.x;
+        f.b = __builtin_amdgcn_readfirstlane(block / (unsigned)groups);
+        f.grp = block - f.b * groups;
         enter_next(f);
         f.t0 = 0;
         f.t1 = f.n_steps;
@@ -818,16 +820,19 @@ __global__ __launch_bounds__(2 * C) void paged_join_kernel(PagedAttnParams p, in
 }
 
 template <typename T, int C, int BIAS, bool PF32, int W, int RT>
-int launch_groups(const PagedAttnParams& p, hipStream_t stream) {
-    const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;
-    if (blocks >= (1LL << 31)) return -1;
+int launch_groups(PagedAttnParams p, hipStream_t stream) {
+    const long long blocks = (long long)p.B * p.Hkv * p.row_tiles;       // at most B H N, below 2^31
     const int rows = p.G * p.N < 16 * RT ? p.G * p.N : 16 * RT;
     if constexpr (group_lds(W, 16 * RT, C) > 65536) {
         static FbLdsOnce once;
         if (!fb_raise_lds_limit((const void*)paged_attn_kernel<T, C, BIAS, PF32, W, RT>, group_lds(W, 16 * RT, C), once)) return 1;
     }
     const size_t lds = group_lds(W, rows, C);
-    hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, W, RT>), dim3((unsigned)blocks), dim3(pa_threads(W)), lds, stream, p);
+    for (long long block0 = 0; block0 < blocks; block0 += kFbLaunchBlocks) {
+        p.block0 = (unsigned)block0;
+        hipLaunchKernelGGL((paged_attn_kernel<T, C, BIAS, PF32, W, RT>), dim3((unsigned)std::min(blocks - block0, kFbLaunchBlocks)),
+                           dim3(pa_threads(W)), lds, stream, p);
+    }
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

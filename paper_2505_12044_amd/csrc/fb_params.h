@@ -77,6 +77,7 @@ struct RotaryParams {
     int pos_f32, pos_shared, interleaved;
     int inverse;             // turn back (the backward)
     int heads_per_group;     // set by the launch
+    long long block0;        // workgroups of the launches before this one
 };
 
 // Pages of a key-value cache.  Requests b = 0..B-1 own ceil(len / page) pages each, table[b][0..).
@@ -105,6 +106,7 @@ struct PagedAppendParams {
     void* phi_pages;         // [n_pages, Hkv, page, R]
     int B, Hkv, N, C, R, page_shift, n_pages;
     int heads_per_group;     // set by the launch
+    long long block0;        // workgroups of the launches before this one
 };
 
 struct PagedAttnParams {
@@ -127,6 +129,7 @@ struct PagedAttnParams {
     float inv_n;             // 1 / N
     int workers;             // waves the keys are split over; 0: a workgroup per key head and row tile, no split
     int waves;               // of such a workgroup, set by the launch
+    unsigned block0;         // such workgroups of the launches before this one
     int joins_by_group;      // joins has an entry per (request, key head, row tile), else one per worker
     float* part_o;           // scratch: two parts per worker, [workers, 2, rows, C], rows = min(tile_rows, H / Hkv * N)
     float* part_m;           // [workers, 2, rows] maxima

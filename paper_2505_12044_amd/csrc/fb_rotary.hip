@@ -14,6 +14,7 @@
 // reaches 4.8); B 8, N 1024, 24 heads, C 64: 12.3 us, 4.1 TB/s; B 8, N 1: 3.9 us.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "fb_device.h"
@@ -45,7 +46,7 @@ FB_DEV void turn(double pos, double freq, float& c, float& s) {
 template <typename T, int VEC, bool INTER>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryParams p) {
     const int units = p.C / (2 * VEC);
-    const long long id = (long long)blockIdx.x * kRotThreads + threadIdx.x;
+    const long long id = (p.block0 + blockIdx.x) * kRotThreads + threadIdx.x;
     const long long token = id / units;
     const int u = (int)(id - token * units);
     if (token >= (long long)p.B * p.N) return;
@@ -124,9 +125,12 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryParams p) {
 }
 
 template <typename T, int VEC>
-void launch_rotary(const RotaryParams& p, dim3 grid, hipStream_t stream) {
-    if (p.interleaved) hipLaunchKernelGGL((rotary_kernel<T, VEC, true>), grid, dim3(kRotThreads), 0, stream, p);
-    else hipLaunchKernelGGL((rotary_kernel<T, VEC, false>), grid, dim3(kRotThreads), 0, stream, p);
+void launch_rotary(RotaryParams& p, long long blocks, unsigned groups, hipStream_t stream) {
+    for (p.block0 = 0; p.block0 < blocks; p.block0 += kFbLaunchBlocks) {
+        const dim3 grid((unsigned)std::min(blocks - p.block0, kFbLaunchBlocks), groups);
+        if (p.interleaved) hipLaunchKernelGGL((rotary_kernel<T, VEC, true>), grid, dim3(kRotThreads), 0, stream, p);
+        else hipLaunchKernelGGL((rotary_kernel<T, VEC, false>), grid, dim3(kRotThreads), 0, stream, p);
+    }
 }
 
 }  // namespace
@@ -144,7 +148,6 @@ int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream) {
     const int vec = (int)(bits & -bits);
     const long long threads = (long long)p.B * p.N * (p.C / (2 * vec));
     const long long blocks = (threads + kRotThreads - 1) / kRotThreads;
-    if (blocks >= (1LL << 31)) return -1;
     // Heads per thread: as many as leave 512 workgroups.  Fewer heads form the angles more often, fewer workgroups leave CUs
     // idle: B 8, N 1024, 24 heads, C 64 on 256, 512, 1024, 2048, 4096 workgroups: 13.5, 12.3, 12.7, 14.6, 18.7 us.
     const int heads = p.H0 + p.H1;
@@ -152,16 +155,15 @@ int fb_launch_rotary(RotaryParams p, bool f32, hipStream_t stream) {
     if (groups > heads) groups = heads;
     p.heads_per_group = (int)((heads + groups - 1) / groups);
     groups = (heads + p.heads_per_group - 1) / p.heads_per_group;
-    const dim3 grid((unsigned)blocks, (unsigned)groups);
     if (f32) {
-        if (vec == 4) launch_rotary<float, 4>(p, grid, stream);
-        else if (vec == 2) launch_rotary<float, 2>(p, grid, stream);
-        else launch_rotary<float, 1>(p, grid, stream);
+        if (vec == 4) launch_rotary<float, 4>(p, blocks, (unsigned)groups, stream);
+        else if (vec == 2) launch_rotary<float, 2>(p, blocks, (unsigned)groups, stream);
+        else launch_rotary<float, 1>(p, blocks, (unsigned)groups, stream);
     } else {
-        if (vec == 8) launch_rotary<bf16_t, 8>(p, grid, stream);
-        else if (vec == 4) launch_rotary<bf16_t, 4>(p, grid, stream);
-        else if (vec == 2) launch_rotary<bf16_t, 2>(p, grid, stream);
-        else launch_rotary<bf16_t, 1>(p, grid, stream);
+        if (vec == 8) launch_rotary<bf16_t, 8>(p, blocks, (unsigned)groups, stream);
+        else if (vec == 4) launch_rotary<bf16_t, 4>(p, blocks, (unsigned)groups, stream);
+        else if (vec == 2) launch_rotary<bf16_t, 2>(p, blocks, (unsigned)groups, stream);
+        else launch_rotary<bf16_t, 1>(p, blocks, (unsigned)groups, stream);
     }
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
