@@ -20,7 +20,8 @@ namespace {
 // table.  A page taken in the same call in which it was given back is looked up where it comes from (a shrinking
 // request's table row, which no one writes), not in the ring, which another workgroup may not have written yet.
 // us for B 64 N 1; B 256 N 4096; B 1024 N 1; B 4096 N 1: with 512 threads and tokens 6.2, 9.8, 9.9, 14.0; 256 each 6.0, 9.6,
-// 10.4, 17.7; 1024 each 6.8, 13.8, 11.2, 13.9.
+// 10.4, 17.7; 1024 each 6.8, 13.8, 11.2, 13.9.  For a prompt's many tokens the scan of the batch, repeated by each of 2048
+// workgroups for one token a thread, is most of the time (B 256 N 4096: 10.3 us for 8.4 MB written).
 constexpr int kPlanThreads = 512;
 constexpr int kPlanItems = 512;
 
@@ -169,7 +170,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
 // ---- new rows into their pages ---------------------------------------------------------------
 // Bound by memory: every row is read once and written once.  A thread owns one vector of one token's rows (its slot is
 // read once) and walks a group of heads, kAppHeads keys and values in flight.  B 8, N 4000 (ragged), 16 heads, C 128 from a
-// fused projection: 90 us, 4.7 TB/s read and written (a large copy reaches 4.8); with 2048 workgroups and more 95 us.
+// fused projection: 89 us, 4.8 TB/s read and written (a copy kernel reaches 5.6, 6.1 with non-temporal loads and stores); with
+// 2048 workgroups and more 95 us.  Factors go element by element, head after head: with rank 2 100 us, rank 16 108 us.
 constexpr int kAppThreads = 256;
 constexpr int kAppHeads = 4;
 

@@ -8,10 +8,10 @@
 // Bound by memory: two numbers in and two out per pair against six multiply-adds.  What could cost more is the angle:
 // positions reach 1e5 and more, where an fp32 product has lost the angle's low digits, so theta is the exact product
 // of two fp32 values in fp64, reduced to an eighth of a turn there, and the rest is fp32 (Taylor polynomials on
-// |theta| <= pi/4, error below 1e-9).  The angle belongs to the token and not to the head: a thread owns VEC pairs of
+// |theta| <= pi/4, cut off below 2e-9 and evaluated in fp32: 6e-8 a rounding).  The angle belongs to the token and not to the head: a thread owns VEC pairs of
 // one token, keeps their sines in registers and walks a group of heads, so each angle is formed once per group.
-// B 4, N 16384, 20 heads, C 128 from a fused projection, three axes: 134 us, 5.0 TB/s read and written (a large copy
-// reaches 4.8); B 8, N 1024, 24 heads, C 64: 12.3 us, 4.1 TB/s; B 8, N 1: 3.9 us.
+// B 4, N 16384, 20 heads, C 128 from a fused projection, three axes: 133 us, 5.1 TB/s read and written (a copy kernel
+// reaches 5.6, 6.1 with non-temporal loads and stores); B 8, N 1024, 24 heads, C 64: 12.2 us, 4.1 TB/s; B 8, N 1: 4.3 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
