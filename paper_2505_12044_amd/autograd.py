@@ -59,14 +59,15 @@ class _FirstOnly(torch.autograd.Function):
 
 
 def _first_only(backward):
-    """A backward whose gradients raise where they are differentiated again (create_graph=True), instead of leaving that
-    part of the second derivative out."""
+    """The backward of a function, from backward(ctx, saved tensors, dout), whose gradients raise where they are differentiated
+    again (create_graph=True), instead of leaving that part of the second derivative out."""
 
     @functools.wraps(backward)
     def call(ctx, dout):
+        saved = ctx.saved_tensors          # (read once: a checkpoint allows no more)
         if not torch.is_grad_enabled():
-            return backward(ctx, dout)
-        return _FirstOnly.apply(lambda: backward(ctx, dout), dout, *ctx.saved_tensors)
+            return backward(ctx, saved, dout)
+        return _FirstOnly.apply(lambda: backward(ctx, saved, dout), dout, *saved)
 
     return call
 
@@ -89,8 +90,8 @@ class _LowRank(torch.autograd.Function):
 
     @staticmethod
     @_first_only
-    def backward(ctx, dout):
-        q, k, v, phi_q, phi_k, out, lse = ctx.saved_tensors
+    def backward(ctx, saved, dout):
+        q, k, v, phi_q, phi_k, out, lse = saved
         causal, scale, cross = ctx.cfg
         dout = _c(dout)
         if cross:
@@ -113,8 +114,8 @@ class _MulBias(torch.autograd.Function):
 
     @staticmethod
     @_first_only
-    def backward(ctx, dout):
-        q, k, v, phi_q, phi_k, out, lse = ctx.saved_tensors
+    def backward(ctx, saved, dout):
+        q, k, v, phi_q, phi_k, out, lse = saved
         causal, scale = ctx.cfg
         dq, dk, dv, dpq, dpk = api.fb_lowrank_mulbias_attn_bwd(q, k, v, phi_q, phi_k, out, lse, _c(dout),
                                                                causal=causal, scale=scale)
@@ -133,8 +134,8 @@ class _Alibi(torch.autograd.Function):
 
     @staticmethod
     @_first_only
-    def backward(ctx, dout):
-        q, k, v, slopes, out, lse = ctx.saved_tensors
+    def backward(ctx, saved, dout):
+        q, k, v, slopes, out, lse = saved
         causal, scale = ctx.cfg
         rows = None
         if ctx.needs_input_grad[3]:
@@ -157,8 +158,8 @@ class _DenseBias(torch.autograd.Function):
 
     @staticmethod
     @_first_only
-    def backward(ctx, dout):
-        q, k, v, bias, out, lse = ctx.saved_tensors
+    def backward(ctx, saved, dout):
+        q, k, v, bias, out, lse = saved
         causal, scale = ctx.cfg
         dq, dk, dv, dbias = api.fb_dense_bias_attn_bwd(q, k, v, bias, out, lse, _c(dout), causal=causal,
                                                        scale=scale)

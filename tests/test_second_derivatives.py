@@ -52,8 +52,7 @@ def device(request, monkeypatch):
     for n in ("lowrank_attn", "lowrank_xattn", "lowrank_mulbias_attn", "alibi_attn", "dense_bias_attn"):
         monkeypatch.setattr(api, f"fb_{n}_fwd", forward)
         monkeypatch.setattr(api, f"fb_{n}_bwd", backward)
-    empty = torch.empty
-    monkeypatch.setattr(torch, "empty", lambda *a, **kw: empty(*a, **kw).zero_())        # the slopes' rows, which no kernel fills
+    monkeypatch.setattr(torch, "empty", torch.zeros)          # the slopes' rows, which no kernel fills
     return "cpu"
 
 
@@ -87,3 +86,14 @@ def test_a_gradient_that_does_not_pass_through_again(device):
     g = torch.autograd.grad((f(*x).float() * w.sum()).sum() + w.square().sum(), (x[0], w), create_graph=True)
     second, = torch.autograd.grad(g[1].sum(), w, retain_graph=True)          # of w's own terms: nothing of the attention's backward
     assert torch.equal(second, torch.full_like(w, 2.0))
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("create_graph", [False, True])
+def test_under_a_checkpoint(device, name, create_graph):
+    """What a recomputed function saved can be read once only."""
+    from torch.utils.checkpoint import checkpoint
+    f, x = make(name, device, True)
+    plain = torch.autograd.grad(f(*x).float().square().sum(), x)
+    again = torch.autograd.grad(checkpoint(f, *x, use_reentrant=False).float().square().sum(), x, create_graph=create_graph)
+    assert all(torch.equal(a, b) for a, b in zip(plain, again))
